@@ -368,6 +368,144 @@ MACKO_API int macko_dense_gemv_group(int n, const void* const* W_dev, const int6
                                      const int64_t* cols, const int64_t* ld, const void* const* x_dev,
                                      void* const* y_dev, void* stream);
 
+/* ---- between the products of a decoder layer: keys and values in 4 bits ---- */
+
+/* What a decoding step does between the products {q,k,v} and {o}: the heads are
+ * normalised (where the model does so) and turned by the position of their token,
+ * keys and values go into a cache, and the queries attend to it.  The cache holds
+ * 4.25 bits a value (OCP microscaling format MXFP4): 32 channels of one token and
+ * head share a byte b, a factor 2^(b-127); each has a 4-bit code, a sign (bit 3)
+ * and one of 0, .5, 1, 1.5, 2, 3, 4, 6.  b is the least one that brings the
+ * largest magnitude to 7 times the factor at most; codes are rounded to nearest,
+ * ties to the even code, and stop at 6.  A group that holds an infinity or a NaN
+ * has b = 255 and reads as NaN.
+ *
+ * 16-bit tensors are fp16 or bf16 (`type`), the same for all of a call; element
+ * d of head h of token t lies at [t * ..._token + h * ..._head + d], strides in
+ * elements (>= 0 for inputs; of outputs no two elements may share a place).
+ * Sums, norms and the softmax are held in 32 bits; results are rounded once.
+ * Row counts, positions, slots, lengths and tables are int32 on the device.
+ * These calls only enqueue on `stream`. */
+typedef enum macko_type { MACKO_FP16 = 0, MACKO_BF16 = 1 } macko_type;
+
+/* A pool of pages.  data_dev: macko_kv_cache_bytes of device memory, 16-byte
+ * aligned, caller owned, of any content: a slot is read only where a caller
+ * says that it holds a token.  page_size: tokens a page, a power of two from 16 to
+ * 4096; head_dim: a multiple of 32 up to 256 (MACKO_E_UNSUPPORTED otherwise).
+ * Slot s is token s % page_size of page s / page_size.  At most 2^31 - 1 slots.
+ * For each page and key/value head, with D = head_dim and n = D / 32:
+ *   key codes    [page_size][D/2]        channel 2i in the low half of byte i
+ *   value codes  [page_size/4][16][4][n] byte [t/4][m][t%4][g]: channel 32g+m in the
+ *                                        low half, 32g+16+m in the high half
+ *   key bytes    [page_size][n]
+ *   value bytes  [page_size][n] */
+typedef struct macko_kv_cache {
+  void* data_dev;
+  int64_t pages;
+  int32_t page_size, kv_heads, head_dim;
+} macko_kv_cache_t;
+
+/* Bytes of such a pool (its data_dev is not looked at), or a negative macko_status. */
+MACKO_API int64_t macko_kv_cache_bytes(const macko_kv_cache_t* cache);
+
+/* Cosines and sines of the positions first .. first + count - 1: table_dev is
+ * float[count][2][rot/2] (cosines, then sines), of angle position * f_i with
+ * f_i = base^(-2i/rot), times `amplitude`.  For contexts longer than a model was
+ * trained on (factor > 1): frequencies that turn r = trained * f_i / 2 pi times
+ * within the trained length keep f_i where r >= high, become f_i / factor where
+ * r <= low, and are blended linearly in r between; high <= low: all become
+ * f_i / factor.  Computed in 64 bits.  rot: even, 2 .. 256. */
+MACKO_API int macko_rope_table(int64_t first, int64_t count, int rot, double base, double factor, double trained,
+                               double low, double high, double amplitude, float* table_dev, void* stream);
+
+/* How heads are turned: the pair (a, b) of channels (i, i + rot/2), or (2i, 2i+1)
+ * if `interleaved`, i < rot/2, becomes (a c - b s, a s + b c) with the cosine and
+ * sine that row positions[t] of the table holds for i; channels from rot on pass.
+ * rot: a multiple of 16 up to head_dim, or 0 (no table, no positions needed).
+ * A weight (head_dim values of `type`, or NULL) first makes every head
+ * x / sqrt(mean(x^2) + eps) * weight. */
+typedef struct macko_rotation {
+  const int32_t* positions_dev; /* [tokens] */
+  const float* table_dev;       /* [table_rows][2][rot/2], 16-byte aligned */
+  int64_t table_rows;
+  int32_t rot, interleaved;
+  float eps;
+} macko_rotation_t;
+
+/* out = the heads of x normalised and turned.  In place (out_dev == x_dev with the same
+ * strides) is fine.  A token whose position lies outside the table gets NaN. */
+MACKO_API int macko_rotate(int64_t tokens, int heads, int head_dim, int type, const void* x_dev, int64_t x_token,
+                           int64_t x_head, const macko_rotation_t* rotation, const void* weight_dev, void* out_dev,
+                           int64_t out_token, int64_t out_head, void* stream);
+
+/* New tokens: q and k are normalised and turned, q goes to q_out, k and v go to
+ * the cache, at slots_dev[t].  A slot below 0 or outside the pool stores nothing
+ * (padding); a position outside the table stores nothing either, and its q_out is NaN.
+ * No two tokens of a call may name the same slot.  heads = 0: no queries.  One launch. */
+typedef struct macko_kv_append_args {
+  int64_t tokens;
+  int32_t heads, type;
+  const void* q_dev;
+  int64_t q_token, q_head;
+  void* q_out_dev;              /* may be q_dev with the same strides */
+  int64_t q_out_token, q_out_head;
+  const void* k_dev;
+  int64_t k_token, k_head;
+  const void* v_dev;
+  int64_t v_token, v_head;
+  const int32_t* slots_dev;     /* [tokens] */
+  const void* q_weight_dev;
+  const void* k_weight_dev;
+  macko_rotation_t rotation;
+} macko_kv_append_args_t;
+MACKO_API int macko_kv_append(const macko_kv_cache_t* cache, const macko_kv_append_args_t* args, void* stream);
+
+/* The values of slots, any number in any order: k_out and v_out [tokens][kv_heads][head_dim] in `type` (either may be
+ * NULL).  A slot below 0 or outside the pool reads as zeros. */
+MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const int32_t* slots_dev, int type,
+                            void* k_out_dev, int64_t k_token, int64_t k_head, void* v_out_dev, int64_t v_token,
+                            int64_t v_head, void* stream);
+
+/* Attention of the queries of `batch` sequences to their cached tokens.  Sequence
+ * b has lengths_dev[b] tokens (below 0 counts as 0), token t in page
+ * tables_dev[b * table_stride + t / page_size]; its queries are the rows
+ * start_dev[b] .. start_dev[b+1] - 1 of q (start_dev NULL: row b), and they are
+ * its last tokens: query i of n is at place p = length - n + i and sees the
+ * tokens t <= p, with a window > 0 only those with t > p - window.  Head h reads
+ * key/value head h / (heads / kv_heads).
+ *   out = sum over seen t of softmax(scale * q.k_t) v_t,   sums = log sum exp(scale * q.k_t)
+ * A query that sees nothing gets zeros and a sum of -infinity.  What lies in
+ * tokens that no query sees, in the rest of pages and in table entries beyond the
+ * length has no effect, NaN included.  A table entry that is needed and names no
+ * page, or is missing (length > table_width * page_size), makes the results of the
+ * queries that need it NaN.
+ * most_queries and longest are upper bounds that size the launch (queries of one
+ * sequence, tokens of one sequence): too small costs time, not correctness.
+ * One launch, two where long sequences are split; workspace_dev:
+ * macko_kv_attention_workspace bytes, 16-byte aligned, of any content, not shared with a call that may
+ * run at the same time (0 bytes: NULL is fine). */
+typedef struct macko_kv_attention_args {
+  int64_t tokens;               /* rows of q */
+  int32_t heads, type, batch;
+  const void* q_dev;
+  int64_t q_token, q_head;
+  void* out_dev;
+  int64_t out_token, out_head;
+  float* sums_dev;              /* [tokens][heads], or NULL */
+  const int32_t* tables_dev;    /* [batch][table_width] */
+  int64_t table_stride;
+  int32_t table_width;
+  const int32_t* lengths_dev;   /* [batch] */
+  const int32_t* start_dev;     /* [batch + 1], from 0 to tokens, or NULL (tokens == batch) */
+  int32_t most_queries, window;
+  int64_t longest;
+  float scale;
+} macko_kv_attention_args_t;
+/* Bytes of workspace for these arguments (pointers are not looked at), or a negative macko_status. */
+MACKO_API int64_t macko_kv_attention_workspace(const macko_kv_cache_t* cache, const macko_kv_attention_args_t* args);
+MACKO_API int macko_kv_attention(const macko_kv_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
+                                 int64_t workspace_bytes, void* stream);
+
 /* ---- housekeeping ---------------------------------------------------------- */
 
 /* Waits until the device is idle if the handle owns device memory (that of the GPU encoder). */

@@ -33,3 +33,4 @@ from .binding import (  # noqa: F401
     wrap_device,
     wrap_device_fp8,
 )
+from .kv import KvCache, rope_table, rotate  # noqa: F401,E402
