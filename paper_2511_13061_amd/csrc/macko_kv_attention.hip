@@ -22,15 +22,22 @@ typedef float V4f __attribute__((ext_vector_type(4)));
 typedef __bf16 B2 __attribute__((ext_vector_type(2)));
 typedef __bf16 B8 __attribute__((ext_vector_type(8)));
 
-constexpr int kWaves = 4, kTile = 32;
+constexpr int kWaves = 4, kTile = 32, kMostSplits = 256;
 constexpr int kMostTokens = 1 << 30;                  // of a sequence: sums of a length and a launch's steps stay in 31 bits
 constexpr float kLift = 8.f;       // how far, in powers of two, a score may pass the running maximum before that moves
 
 struct Grid {
   int32_t row_blocks, splits;      // of a sequence's rows and of its tokens, at most
+  int32_t ordered;                 // long sequences first
   int64_t chunk;                   // tokens of a split, at least; a multiple of kWaves * kTile
   float* parts;                    // [tokens * heads][splits][D], then [tokens * heads][splits][2]: maximum and sum
 };
+
+struct Launch {
+  KvAttention a;
+  Grid g;
+};
+typedef const __attribute__((address_space(4))) Launch* LaunchPtr;
 
 struct Sequence {
   int length, first, queries, rows;
@@ -63,6 +70,20 @@ __device__ inline Span span_of(const KvAttention& a, const Grid& g, const Sequen
   return p;
 }
 
+__device__ inline int later(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The sequence that is n-th by length, longest first (at most 64 of them): workgroups start in this order, and the last ones to end are short.
+__device__ inline int nth_longest(const KvAttention& a, int n, int lane) {
+  const int key = lane < a.batch ? min(max(a.lengths[lane], 0), (1 << 25) - 1) * 64 + 63 - lane : -1;
+  int longer = 0;
+#pragma unroll
+  for (int m = 0; m < 64; ++m) longer += __builtin_amdgcn_readlane(key, m) > key;
+  return __builtin_ctzll(__ballot(longer == n && lane < a.batch));
+}
+
 // What a wavefront holds of 32 tokens: two blocks of 16.
 template <int NG>
 struct Tile {
@@ -87,39 +108,102 @@ __device__ inline B2 decode_at(uint32_t word, uint32_t bytes, int at) {
   }
 }
 
+// Wavefronts on a SIMD that the registers are to leave room for.
+constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? (ng <= 4 ? 2 : 1) : ng == 1 ? 4 : ng <= 4 ? 3 : 1; }
+
 template <int NG, bool BF, int RT>
-__global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttention a, const Grid g) {
+__global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_kernel(const Launch args) {
+  const KvAttention& a = args.a;
+  const Grid& g = args.g;
   constexpr int D = 32 * NG, NK = (NG + 3) / 4, NP = BF ? 2 : 3, R = 16 * RT, LD = D + 4;
-  extern __shared__ __align__(16) float lds[];           // [kWaves][16][LD], then maxima and sums [kWaves][16] each
+  extern __shared__ __align__(16) float lds[];           // [kWaves][16][LD], maxima and sums [kWaves][16] each, and below
   float* const lds_max = lds + kWaves * 16 * LD;
   float* const lds_sum = lds_max + kWaves * 16;
+  uint32_t* const lds_spoilt = reinterpret_cast<uint32_t*>(lds_sum + kWaves * 16);      // [RT][kWaves][16]: groups in which a row sees what is not a number
 
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t pairs = (uint32_t)a.batch * a.pool.heads, bh = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int b = (int)(bh / a.pool.heads), head = (int)(bh % a.pool.heads), split = (int)(rest / g.row_blocks);
+  const int head = (int)(bh % a.pool.heads), split = (int)(rest / g.row_blocks);
+  int b = (int)(bh / a.pool.heads);
+  if (g.ordered) b = nth_longest(a, b, threadIdx.x & 63);
   const Sequence seq = sequence_of(a, b);
   const int32_t* const table = a.tables + b * a.table_stride;
   const int64_t piece = kv_piece_bytes(int64_t{1} << a.pool.page_bits, D), page_stride = piece * a.pool.heads;
   const uint8_t* const pool = a.pool.data + head * piece;
   const int page_size = 1 << a.pool.page_bits;
-  const float scale = a.scale * 1.4426950408889634f;     // weights are powers of two
+  // Weights are 2^(score * unit - maximum); the scale's sign goes into the queries, so that the largest score has the largest weight.
+  const float unit = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f, sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
+  const float lift = kLift / unit;
+  const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
   for (int first_row = (int)(rest % g.row_blocks) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
     const Span span = span_of(a, g, seq, first_row, R);
     if (split >= span.used) continue;
+    // What follows from the lane is worked out here and again behind the steps (later(...)): kept from outside the loop it would hold registers.
+    const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4;
     const int begin = span.lo + split * span.chunk, end = min(span.hi, begin + span.chunk);
 
+    bool bad = end > begin && (a.table_width == 0 || a.pool.pages == 0);     // a page that is needed is missing
+    const int last_block = (end - 1) >> 4;
+    float top[RT], sum[RT];
+    V4f out[RT][2 * NG];
+
+    // A lane holds the page of one block of the wavefront's next 32 steps: one load for all of them, ahead of the loads that need it.
+    int pages = 0;
+    auto look_up = [&](int at) {
+      const int block = min((at >> 4) + (lane >> 1) * (kWaves * 2) + (lane & 1), last_block), index = block >> (a.pool.page_bits - 4);
+      const int page = table[min(index, a.table_width - 1)];
+      const bool fine = index < a.table_width && page >= 0 && page < a.pool.pages;
+      bad = bad || __any(!fine);
+      pages = fine ? page : 0;
+    };
+    const uint32_t key_lane = n * (D / 2) + j * 16, key_byte_lane = n * NG + j, value_lane = (j * 16 + n) * (4 * NG), value_byte_lane = j * (4 * NG);
+    auto load = [&](Tile<NG>& t, int at, int slot) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int block = min((at >> 4) + u, last_block), in_page = (block << 4) & (page_size - 1);
+        const uint8_t* const codes = pool + (int64_t)__builtin_amdgcn_readlane(pages, slot * 2 + u) * page_stride + in_page * (D / 2);
+        const uint8_t* const bytes = codes + page_size * D - in_page * (D / 2 - NG);
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+          const int group = kk * 4 + j;
+          t.key[u][kk] = V4i{0, 0, 0, 0};
+          t.key_byte[u][kk] = 0;
+          if (group < NG) {
+            t.key[u][kk] = *reinterpret_cast<const V4i*>(codes + key_lane + kk * 64);
+            t.key_byte[u][kk] = bytes[key_byte_lane + kk * 4];
+          }
+        }
+        const uint32_t* const v = reinterpret_cast<const uint32_t*>(codes + page_size * (D / 2) + value_lane);
+        const uint32_t* const vb = reinterpret_cast<const uint32_t*>(bytes + page_size * NG + value_byte_lane);
+#pragma unroll
+        for (int w = 0; w < NG; ++w) {
+          t.value[u][w] = v[w];
+          t.value_byte[u][w] = vb[w];
+        }
+      }
+    };
+    Tile<NG> one, two;
+    const int mine = begin + wave * kTile;                // the wavefront's first step
+    const bool any = mine < end && !bad;
+    if (any) {                                            // on its way while the queries are made ready
+      look_up(mine);
+      load(one, mine, 0);
+    }
+
     // rows of this lane
-    int see_lo[RT], see_hi[RT];
+    if (lane < 16) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) lds_spoilt[(rt * kWaves + wave) * 16 + lane] = 0;
+    }
+    int place[RT];                                        // of a row's query: it sees the tokens t with 0 <= place - t < reach
     V8i q[RT][NK][NP];
     int q_byte[RT][NK];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int row = first_row + rt * 16 + n, query = row / a.shared;
       const bool there = row < seq.rows;
-      const int at = seq.length - seq.queries + query;
-      see_hi[rt] = there ? min(max(at + 1, 0), seq.length) : 0;
-      see_lo[rt] = a.window ? max(at - a.window + 1, 0) : 0;
+      place[rt] = there ? seq.length - seq.queries + query : -1;
       const uint16_t* src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
@@ -140,9 +224,9 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
           for (int i = 0; i < 16; ++i) most = max(most, __builtin_bit_cast(uint32_t, x[u][i]) & 0x7FFFFFFFu);
           most = max(most, (uint32_t)__shfl_xor((int)most, 16));      // two lanes share a group
           top[u] = max(most >> 23, 20u) - 7u;             // largest magnitude to [128, 256)
-          const float unit = __builtin_bit_cast(float, (254u - top[u]) << 23);
+          const float up = __builtin_bit_cast(float, (254u - top[u]) << 23) * sign;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[u][i] *= unit;
+          for (int i = 0; i < 16; ++i) x[u][i] *= up;
 #pragma unroll
           for (int p = 0; p < NP; ++p) {
 #pragma unroll
@@ -165,47 +249,6 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
       }
     }
 
-    bool bad = end > begin && (a.table_width == 0 || a.pool.pages == 0);     // a page that is needed is missing
-    const int last_block = (end - 1) >> 4;
-    float top[RT], sum[RT];
-    V4f out[RT][2 * NG];
-    uint32_t spoilt[RT];                                  // groups in which a seen value is not a number
-
-    auto page_of = [&](int block) {
-      const int index = min(block, last_block) >> (a.pool.page_bits - 4);
-      const int page = table[min(index, a.table_width - 1)];
-      const bool fine = index < a.table_width && page >= 0 && page < a.pool.pages;
-      bad = bad || !fine;
-      return fine ? page : 0;
-    };
-    auto load = [&](Tile<NG>& t, int at) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int block = min((at >> 4) + u, last_block), in_page = (block << 4) & (page_size - 1);
-        const uint8_t* const codes = pool + (int64_t)page_of(block) * page_stride;
-        const uint8_t* const keys = codes + in_page * (D / 2);
-        const uint8_t* const values = codes + page_size * (D / 2) + in_page * (D / 2);
-        const uint8_t* const key_bytes = codes + page_size * D + in_page * NG;
-        const uint8_t* const value_bytes = codes + page_size * (D + NG) + in_page * NG;
-#pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-          const int group = kk * 4 + j;
-          t.key[u][kk] = V4i{0, 0, 0, 0};
-          t.key_byte[u][kk] = 0;
-          if (group < NG) {
-            t.key[u][kk] = *reinterpret_cast<const V4i*>(keys + n * (D / 2) + group * 16);
-            t.key_byte[u][kk] = key_bytes[n * NG + group];
-          }
-        }
-        const uint32_t* const v = reinterpret_cast<const uint32_t*>(values + (j * 16 + n) * (4 * NG));
-        const uint32_t* const vb = reinterpret_cast<const uint32_t*>(value_bytes + j * (4 * NG));
-#pragma unroll
-        for (int w = 0; w < NG; ++w) {
-          t.value[u][w] = v[w];
-          t.value_byte[u][w] = vb[w];
-        }
-      }
-    };
     auto step = [&](Tile<NG>& t, int at, bool careful) {
       const bool masked = at < span.all_lo || at + kTile > span.all_hi;
       B8 p_hi[RT], p_lo[RT];
@@ -223,31 +266,31 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
             s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q[rt][kk][0], s, 4, 0, 0, t.key_byte[u][kk], 0, q_byte[rt][kk]);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[4 * u + i] = s[i] * scale;
+          for (int i = 0; i < 4; ++i) x[4 * u + i] = s[i];
         }
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int token = at + (i >> 2) * 16 + j * 4 + (i & 3);
-            if (token < see_lo[rt] || token >= see_hi[rt]) x[i] = -INFINITY;
+            if ((uint32_t)(place[rt] - token) >= reach) x[i] = -INFINITY;
           }
         }
         const float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__any(most > top[rt] + kLift)) {
+        if (__any(most > top[rt] + lift)) {
           float to = fmaxf(most, __shfl_xor(most, 16));
           to = fmaxf(to, __shfl_xor(to, 32));
           to = fmaxf(to, top[rt]);
-          const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f(top[rt] - to);
+          const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
           top[rt] = to;
           sum[rt] *= by;
 #pragma unroll
           for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
         }
-        const float base = top[rt] == -INFINITY ? 0.f : top[rt];       // nothing seen yet: weights of 2^-inf, not NaN
+        const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;       // nothing seen yet: weights of 2^-inf, not NaN
         uint32_t bits[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float w = __builtin_amdgcn_exp2f(x[i] - base);
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
           sum[rt] += w;
           bits[i] = __builtin_bit_cast(uint32_t, w);
         }
@@ -281,7 +324,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
               if (careful && nan) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                  if (token >= see_lo[rt] && token < see_hi[rt]) spoilt[rt] |= 1u << i;
+                  if ((uint32_t)(place[rt] - token) < reach) atomicOr(lds_spoilt + (rt * kWaves + wave) * 16 + n, 1u << i);
               }
             }
           }
@@ -316,24 +359,31 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
       for (int rt = 0; rt < RT; ++rt) {
         top[rt] = -INFINITY;
         sum[rt] = 0.f;
-        spoilt[rt] = 0;
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c) out[rt][c] = V4f{0.f, 0.f, 0.f, 0.f};
       }
-      int at = begin + wave * kTile;
-      if (at < end && !bad) {
-        Tile<NG> one, two;
-        load(one, at);
+      if (any) {
+        int at = mine, slot = 0;
+        if (pass > 0) {
+          look_up(at);
+          load(one, at, 0);
+        }
+        auto ahead = [&](Tile<NG>& t, int next) {
+          if (next >= end) return;
+          if (++slot == 32) {
+            look_up(next);
+            slot = 0;
+          }
+          load(t, next, slot);
+        };
         for (;;) {
-          int next = at + kWaves * kTile;
-          if (next < end) load(two, next);
+          ahead(two, at + kWaves * kTile);
           step(one, at, pass > 0);
-          at = next;
+          at += kWaves * kTile;
           if (at >= end) break;
-          next = at + kWaves * kTile;
-          if (next < end) load(one, next);
+          ahead(one, at + kWaves * kTile);
           step(two, at, pass > 0);
-          at = next;
+          at += kWaves * kTile;
           if (at >= end) break;
         }
       }
@@ -349,28 +399,32 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
       if (!__any(nan)) break;
     }
 
+    // What the results need of the arguments is read again here, rather than kept in registers through the steps.
+    LaunchPtr e = (LaunchPtr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(e));
+    const int rows_of_sequence = seq.rows, first_of_sequence = seq.first;
+    const int thread = later(threadIdx.x), row16 = thread & 15, quad = thread >> 4 & 3;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       sum[rt] += __shfl_xor(sum[rt], 16);
       sum[rt] += __shfl_xor(sum[rt], 32);
       if (bad) sum[rt] = NAN;
-      spoilt[rt] |= (uint32_t)__shfl_xor((int)spoilt[rt], 16);
-      spoilt[rt] |= (uint32_t)__shfl_xor((int)spoilt[rt], 32);
-      float* const mine = lds + (wave * 16 + n) * LD;
+      const uint32_t spoilt = lds_spoilt[(rt * kWaves + wave) * 16 + row16];
+      float* const mine = lds + (wave * 16 + row16) * LD;
 #pragma unroll
       for (int c = 0; c < 2 * NG; ++c) {
         V4f o = out[rt][c];
-        if (spoilt[rt] >> (c / 2) & 1) o = V4f{NAN, NAN, NAN, NAN};
-        *reinterpret_cast<V4f*>(mine + c * 16 + j * 4) = o;
+        if (spoilt >> (c / 2) & 1) o = V4f{NAN, NAN, NAN, NAN};
+        *reinterpret_cast<V4f*>(mine + c * 16 + quad * 4) = o;
       }
-      if (j == 0) {
-        lds_max[wave * 16 + n] = top[rt];
-        lds_sum[wave * 16 + n] = sum[rt];
+      if (quad == 0) {
+        lds_max[wave * 16 + row16] = top[rt] * unit;
+        lds_sum[wave * 16 + row16] = sum[rt];
       }
       __syncthreads();
-      for (int item = threadIdx.x; item < 4 * D; item += 64 * kWaves) {
+      for (int item = thread; item < 4 * D; item += 64 * kWaves) {
         const int r = item / (D / 4), channel = item % (D / 4) * 4, row = first_row + rt * 16 + r;
-        if (row >= seq.rows) continue;
+        if (row >= rows_of_sequence) continue;
         float most = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) most = fmaxf(most, lds_max[w * 16 + r]);
@@ -382,23 +436,23 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(const KvAttentio
           total += lds_sum[w * 16 + r] * by;
           o += *reinterpret_cast<const V4f*>(lds + (w * 16 + r) * LD + channel) * by;
         }
-        const int query = row / a.shared, h = head * a.shared + row - query * a.shared;
-        const int64_t token = seq.first + query;
+        const int query = row / e->a.shared, h = head * e->a.shared + row - query * e->a.shared;
+        const int64_t token = first_of_sequence + query;
         if (span.used > 1) {
-          const int64_t part = (token * a.heads + h) * g.splits + split;
-          *reinterpret_cast<V4f*>(g.parts + part * D + channel) = o;
+          const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
+          *reinterpret_cast<V4f*>(e->g.parts + part * D + channel) = o;
           if (channel == 0) {
-            float* const ms = g.parts + a.tokens * a.heads * g.splits * D + part * 2;
+            float* const ms = e->g.parts + e->a.tokens * e->a.heads * e->g.splits * D + part * 2;
             ms[0] = most;
             ms[1] = total;
           }
           continue;
         }
         const float r1 = total == 0.f ? 0.f : 1.f / total;
-        uint16_t* const dst = reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + h * a.out_head + channel;
+        uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + channel;
 #pragma unroll
         for (int i = 0; i < 4; ++i) dst[i] = (uint16_t)to_bits<BF>(o[i] * r1);
-        if (a.sums && channel == 0) a.sums[token * a.heads + h] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+        if (e->a.sums && channel == 0) e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
       }
       __syncthreads();
     }
@@ -410,8 +464,14 @@ template <int NG, bool BF, int RT>
 __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Grid g) {
   constexpr int D = 32 * NG, R = 16 * RT, LANES = D / 4, GROUPS = 256 / LANES;      // a group of lanes takes a split at a time
   __shared__ __align__(16) float lds[GROUPS][D];
-  __shared__ float lds_sum[GROUPS];
+  __shared__ float weight[kMostSplits], most_of[4], total_of[4];
   const int64_t id = blockIdx.x;
+  const float* const parts = g.parts + id * g.splits * D;
+  const float* const ms = g.parts + a.tokens * a.heads * g.splits * D + id * g.splits * 2;
+  const int mine = threadIdx.x, wave = mine >> 6, group = mine / LANES, channel = mine % LANES * 4;
+  // on their way before it is known how many splits there are
+  float my_top = 0.f, my_sum = 0.f;
+  if (mine < g.splits) my_top = ms[2 * mine], my_sum = ms[2 * mine + 1];
   const int h = (int)(id % a.heads), head = h / a.shared;
   const int64_t token = id / a.heads;
   // the sequence of a token
@@ -431,31 +491,32 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
   const int row = query * a.shared + h - head * a.shared;
   const Span span = span_of(a, g, seq, row / R * R, R);
   if (span.used <= 1) return;
-  const float* const parts = g.parts + id * g.splits * D;
-  const float* const ms = g.parts + a.tokens * a.heads * g.splits * D + id * g.splits * 2;
-  float most = -INFINITY;
-  for (int s = 0; s < span.used; ++s) most = fmaxf(most, ms[2 * s]);
-  const int group = threadIdx.x / LANES, channel = threadIdx.x % LANES * 4;
+  static_assert(kMostSplits == 256, "a thread has one split's maximum");
+  const bool has = mine < span.used;
+  const float top = has ? my_top : -INFINITY;
+  float most = top;
+  for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+  if ((mine & 63) == 0) most_of[wave] = most;
+  __syncthreads();
+  most = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
+  const float by = top == most ? 1.f : __builtin_amdgcn_exp2f(top - most);
+  weight[mine] = by;
+  float total = has ? my_sum * by : 0.f;
+  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+  if ((mine & 63) == 0) total_of[wave] = total;
+  __syncthreads();
+  V4f o = {0.f, 0.f, 0.f, 0.f};
   if (group < GROUPS) {
-    V4f o = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-    for (int s = group; s < span.used; s += GROUPS) {
-      const float by = ms[2 * s] == most ? 1.f : __builtin_amdgcn_exp2f(ms[2 * s] - most);
-      total += ms[2 * s + 1] * by;
-      o += *reinterpret_cast<const V4f*>(parts + (int64_t)s * D + channel) * by;
-    }
+#pragma unroll 4
+    for (int s = group; s < span.used; s += GROUPS) o += *reinterpret_cast<const V4f*>(parts + (int64_t)s * D + channel) * weight[s];
     *reinterpret_cast<V4f*>(&lds[group][channel]) = o;
-    if (channel == 0) lds_sum[group] = total;
   }
   __syncthreads();
   if (group > 0) return;
-  V4f o = {0.f, 0.f, 0.f, 0.f};
-  float total = 0.f;
+  o = V4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < GROUPS; ++k) {
-    o += *reinterpret_cast<const V4f*>(&lds[k][channel]);
-    total += lds_sum[k];
-  }
+  for (int k = 0; k < GROUPS; ++k) o += *reinterpret_cast<const V4f*>(&lds[k][channel]);
+  total = (total_of[0] + total_of[1]) + (total_of[2] + total_of[3]);
   const float r1 = total == 0.f ? 0.f : 1.f / total;
   uint16_t* const dst = reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + h * a.out_head + channel;
 #pragma unroll
@@ -470,21 +531,22 @@ Grid grid_of(const KvAttention& a) {
   Grid g{};
   const int64_t rows = 16 * row_tiles(a), unit = kWaves * kTile;
   g.row_blocks = (int32_t)(((int64_t)a.most_queries * a.shared + rows - 1) / rows);
-  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, wanted = (int64_t)device_cu_count() * 4;
+  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, wanted = (int64_t)device_cu_count() * 2;
   const int64_t longest = std::max<int64_t>(1, std::min(a.longest, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest));
   int64_t splits = others > 0 ? (wanted + others - 1) / others : 1;
   splits = std::max<int64_t>(1, std::min({splits, (longest + 4 * unit - 1) / (4 * unit), (int64_t)256}));
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
   g.splits = (int32_t)((longest + g.chunk - 1) / g.chunk);
+  g.ordered = a.batch > 1 && a.batch <= 64 && others * g.splits > 3 * (int64_t)device_cu_count();
   return g;
 }
 
 template <int NG, bool BF, int RT>
 int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
-  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + 2 * kWaves * 16);
+  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + (2 + RT) * kWaves * 16);
   const int64_t blocks = (int64_t)a.batch * a.pool.heads * g.row_blocks * g.splits, rows = a.tokens * a.heads;
   if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<NG, BF, RT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-  hipLaunchKernelGGL((attention_kernel<NG, BF, RT>), dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, a, g);
+  hipLaunchKernelGGL((attention_kernel<NG, BF, RT>), dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, Launch{a, g});
   MACKO_HIP_TRY(hipGetLastError());
   if (g.splits > 1) {
     hipLaunchKernelGGL((join_kernel<NG, BF, RT>), dim3((unsigned)rows), dim3(256), 0, stream, a, g);
