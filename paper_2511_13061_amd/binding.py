@@ -157,7 +157,9 @@ def load_library():
     from . import kv
     kv._declare(lib)
     if native is not None:
-        native.bind(*[ctypes.cast(f, vp).value for f in (lib.macko_spmv, lib.macko_spmm, lib.macko_decode_device)])
+        native.bind(*[ctypes.cast(f, vp).value for f in (
+            lib.macko_spmv, lib.macko_spmm, lib.macko_decode_device, lib.macko_rotate, lib.macko_kv_append, lib.macko_kv_read,
+            lib.macko_kv_attention_workspace, lib.macko_kv_attention)])
         _native = native
     _lib = lib
     return lib

@@ -9,7 +9,7 @@ import ctypes
 import math
 
 from . import binding
-from .binding import _check, _dev_ptr, _need_torch, _stream_ptr, load_library
+from .binding import _check, _dev_ptr, _made, _need_torch, _stream_ptr, load_library
 
 _i32, _i64, _vp, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
 
@@ -143,6 +143,10 @@ def rotate(x, positions, table, weight=None, eps=1e-6, interleaved=False, out=No
     """macko_rotate: the heads x [tokens, heads, head_dim] normalised (with a weight [head_dim]) and turned by their tokens' positions.
 
     positions: int32 [tokens], rows of the table (rope_table); table None: the norm alone.  `out` may be x."""
+    if stream is None and binding._native is not None:
+        y = binding._native.rotate(x, positions, table, weight, eps, interleaved, out)
+        if y is not None:                    # None: something to be refused, a forked child or anything out of the ordinary
+            return _made(y, "macko_rotate")
     torch = _need_torch()
     kind = _type_of(x)
     src = _heads(x, "x", x.shape)
@@ -176,11 +180,16 @@ class KvCache:
             raise ValueError(f"data must be a contiguous {list(shape)} tensor on the GPU")
         c.data = data.data_ptr()
         self.data, self._c, self._p = data, c, ctypes.byref(c)
+        self._address, self._device = ctypes.addressof(c), data.device.index
         self.pages, self.page_size, self.kv_heads, self.head_dim = c.pages, c.page_size, c.kv_heads, c.head_dim
 
     def append(self, q, k, v, positions, slots, table=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, q_out=None, stream=None):
         """macko_kv_append: q and k [tokens, heads, head_dim] normalised (weights) and turned (table, positions), k and v into the slots
         (int32 [tokens], below 0: none).  Returns q_out, which may be q; None without queries."""
+        if stream is None and binding._native is not None:
+            y = binding._native.kv_append(self._address, self._device, q, k, v, positions, slots, table, q_weight, k_weight, eps, interleaved, q_out)
+            if y is not None:
+                return None if y is True else _made(y, "macko_kv_append")
         torch = _need_torch()
         kind, tokens = _type_of(k), k.shape[0]
         shape = (tokens, self.kv_heads, self.head_dim)
@@ -204,9 +213,15 @@ class KvCache:
 
     def read(self, slots, dtype=None, k_out=None, v_out=None, stream=None):
         """macko_kv_read: keys and values [tokens, kv_heads, head_dim] of the slots (int32, below 0: zeros), in dtype (float16 by default)."""
-        torch = _need_torch()
+        torch = binding._torch or _need_torch()
+        if dtype is None:
+            given = k_out if k_out is not None else v_out
+            dtype = torch.float16 if given is None else given.dtype
+        if stream is None and binding._native is not None and (dtype == torch.float16 or dtype == torch.bfloat16):
+            pair = binding._native.kv_read(self._address, self._device, slots, dtype == torch.bfloat16, k_out, v_out)
+            if pair is not None:
+                return _made(pair, "macko_kv_read")
         shape = (slots.shape[0], self.kv_heads, self.head_dim)
-        dtype = dtype or (k_out if k_out is not None else v_out if v_out is not None else torch.empty(0, dtype=torch.float16)).dtype
         with _on(self.data, stream):
             made = [torch.empty(shape, dtype=dtype, device=self.data.device) if x is None else x for x in (k_out, v_out)]
             if made[0].dtype != dtype:
@@ -225,6 +240,10 @@ class KvCache:
         the rows of q that are each sequence's, up to most_queries; None: one row a sequence.  longest: a bound on the lengths, of all
         that the tables can hold unless given.  scale: head_dim ** -0.5 unless given.  Returns out, or (out, sums) with sums = True:
         float32 [tokens, heads], the logarithm of each row's sum, to join results over parts of a context."""
+        if stream is None and binding._native is not None:
+            y = binding._native.kv_attend(self._address, self._device, q, tables, lengths, start, most_queries, longest, scale, window, sums, out)
+            if y is not None:
+                return _made(y, "macko_kv_attention")
         torch = _need_torch()
         if q.dim() != 3:
             raise ValueError("q must be [tokens, heads, head_dim]")

@@ -516,7 +516,10 @@ def test_a_decoding_step_in_a_graph():
 
 # ---- refusals -----------------------------------------------------------------
 
-def test_refusals_of_the_python_calls():
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals_of_the_python_calls(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(M.binding, "_native", None)
     cache = M.KvCache(4, 16, 2, 64)
     x = torch.zeros((3, 2, 64), dtype=torch.float16, device="cuda")
     i3, tab = ints([0, 1, 2]), M.rope_table(8, 64)
@@ -549,3 +552,38 @@ def test_refusals_of_the_python_calls():
     assert [t.shape[0] for t in cache.read(i3[:0])] == [0, 0]
     assert cache.attend(x[:0], one[:0], i3[:0]).shape == (0, 2, 64)
     assert cache.attend(x[:0], one, i3, start=ints([0, 0, 0, 0])).shape == (0, 2, 64)
+
+
+def test_native_calls_do_what_the_general_ones_do(monkeypatch):
+    M.load_library()
+    native = M.binding._native
+    assert native is not None
+    g = rng(31)
+    page, dim, heads, kv_heads, tokens = 16, 64, 4, 2, 9
+    tab, at, slots = M.rope_table(50, dim), ints(np.arange(9) * 5), ints(np.arange(9) * 3)
+    w = normal(g, dim).cuda()
+    x = normal(g, tokens, heads + 2 * kv_heads, dim).cuda()
+    q, k, v = x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]
+    table, lengths, start = ints([[0, 1, -1], [0, 1, 1]]), ints([20, 31]), ints([0, 3, 9])
+    kept = torch.zeros((tokens, heads, dim), dtype=torch.float16, device="cuda")
+    b = x.bfloat16()
+    calls = [
+        lambda c: M.rotate(q, at, tab), lambda c: M.rotate(q, at, tab, w, 1e-3, True), lambda c: M.rotate(q, None, None, weight=w), lambda c: M.rotate(q, at, tab, out=kept) is kept,
+        lambda c: M.rotate(b, at, tab, weight=w.bfloat16()), lambda c: M.rotate(q.transpose(0, 1), ints([1, 2, 3, 4]), tab),
+        lambda c: c.append(q, k, v, at, slots, tab, q_weight=w, k_weight=w, eps=1e-4, interleaved=True), lambda c: c.append(None, k, v, None, slots),
+        lambda c: c.append(q, k, v, at, slots, tab, q_out=kept) is kept, lambda c: kept.clone(), lambda c: c.append(b[:, :4], b[:, 4:6], b[:, 6:], at, slots, tab),
+        lambda c: c.read(slots), lambda c: c.read(slots, torch.bfloat16), lambda c: c.read(slots, k_out=kept[:, :2])[0].data_ptr() == kept.data_ptr(),
+        lambda c: c.attend(q, table, lengths, start=start, most_queries=6, window=11, scale=-0.2, sums=True), lambda c: c.attend(q[:2], table, lengths),
+        lambda c: c.attend(q[:2], table, lengths, longest=31, out=kept[:2]) is not None, lambda c: kept.clone(), lambda c: c.attend(b[:2, :4], table, lengths, sums=True),
+        lambda c: c.attend(q[:2], table, lengths, scale=0.0), lambda c: c.attend(q[:0], table[:0], lengths[:0]), lambda c: c.data.clone(),
+    ]
+    results = []
+    for part in (native, None):
+        monkeypatch.setattr(M.binding, "_native", part)
+        cache = M.KvCache(3, page, kv_heads, dim, data=torch.zeros((3, kv_heads, ref.piece_bytes(page, dim)), dtype=torch.uint8, device="cuda"))
+        kept.zero_()
+        results.append([call(cache) for call in calls])
+    for i, (one, two) in enumerate(zip(*results)):
+        for a, c in zip(one if isinstance(one, tuple) else (one,), two if isinstance(two, tuple) else (two,)):
+            assert type(a) is type(c), i
+            assert (torch.equal(a, c) and a.dtype == c.dtype) if isinstance(a, torch.Tensor) else a == c, i
