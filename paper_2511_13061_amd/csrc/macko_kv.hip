@@ -12,28 +12,29 @@ namespace macko {
 namespace {
 
 constexpr int kBlock = 256;
+typedef float V4 __attribute__((ext_vector_type(4)));
 constexpr int64_t kMostBlocks = (int64_t{1} << 24) - 1;  // a launch has fewer than 2^32 threads
 
 struct Heads {
   const uint16_t* x;
   int64_t token, head;       // strides in elements
+  const uint16_t* weight;
+  int32_t heads;
+  int32_t bundles;           // of a token: heads that a group of lanes takes together
+  int64_t blocks;            // that the launch has for these heads
 };
 struct TurnArgs {
-  Heads q, k, v;
+  Heads part[3];             // queries, keys, values
   uint16_t* out;
   int64_t out_token, out_head;
-  const uint16_t* q_weight;
-  const uint16_t* k_weight;
   const int32_t* positions;
   const int32_t* slots;
   const float* table;
   int64_t table_rows;
-  KvPool pool;               // heads = 0: queries alone
-  int64_t items, slots_held; // heads of all tokens; slots of the pool
-  int32_t heads, all_heads;  // query heads; with key and value heads
+  KvPool pool;
+  int64_t tokens, slots_held, blocks;
   int32_t dim, rot, interleaved;
   int32_t lane_bits;         // log2 of the lanes of a head
-  int32_t rounds;            // heads that a group of lanes takes one after the other
   float eps;
 };
 
@@ -44,15 +45,10 @@ __device__ inline float group_sum(float x, int lanes) {
 
 // The 4-bit codes of 8 channels of a group that 4 neighbouring lanes hold, 2 to a byte, and the group's byte.
 __device__ inline uint32_t encode8(const float* y, uint32_t* byte) {
-  float most = 0.f;
-  bool finite = true;
+  uint32_t bits = 0;                                     // magnitudes are ordered as their bits are, infinities and NaN above all
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    most = fmaxf(most, fabsf(y[i]));
-    finite = finite && fabsf(y[i]) < INFINITY;           // false for a NaN
-  }
-  uint32_t bits = finite ? __builtin_bit_cast(uint32_t, most) : 0x7F800000u;
-  bits = max(bits, (uint32_t)__shfl_xor((int)bits, 1));  // magnitudes are ordered as their bits are
+  for (int i = 0; i < 8; ++i) bits = max(bits, __builtin_bit_cast(uint32_t, y[i]) & 0x7FFFFFFFu);
+  bits = max(bits, (uint32_t)__shfl_xor((int)bits, 1));
   bits = max(bits, (uint32_t)__shfl_xor((int)bits, 2));
   // the exponent of most / 7, rounded up: 7 = 1.75 * 2^2, and a mantissa above 1.75 carries
   const uint32_t e = (bits + 0x1FFFFFu) >> 23;
@@ -67,118 +63,139 @@ __device__ inline uint32_t encode8(const float* y, uint32_t* byte) {
   return word;
 }
 
-template <bool BF>
+// Lanes 4g + 2u + v hold the codes of channels 32g + 16u + 8v + e as keys are stored, 8 of them in a word; a byte of the values' layout takes
+// the same e from u = 0 and u = 1.  The word of lane 4g + 2u + v here: bytes m = 8v + 4u + (0 .. 3) of group g.  And back.
+__device__ inline uint32_t pair_values(uint32_t word, bool upper) {
+  const uint32_t far = (uint32_t)__shfl_xor((int)word, 2);
+  const uint32_t low = upper ? far >> 16 : word & 0xFFFFu, high = upper ? word >> 16 : far & 0xFFFFu;
+  // 4 codes to the low halves of 4 bytes, 4 to the high ones
+  const uint32_t a = (low | low << 8) & 0x00FF00FFu, b = (high | high << 8) & 0x00FF00FFu;
+  return ((a | a << 4) & 0x0F0F0F0Fu) | ((b | b << 4) & 0x0F0F0F0Fu) << 4;
+}
+__device__ inline uint32_t unpair_values(uint32_t word, bool upper) {
+  uint32_t a = word & 0x0F0F0F0Fu, b = word >> 4 & 0x0F0F0F0Fu;
+  a = (a | a >> 4) & 0x00FF00FFu, b = (b | b >> 4) & 0x00FF00FFu;
+  a = (a | a >> 8) & 0xFFFFu, b = (b | b >> 8) & 0xFFFFu;
+  const uint32_t give = upper ? a : b, far = (uint32_t)__shfl_xor((int)give, 2);
+  return upper ? far | b << 16 : a | far << 16;
+}
+// A 4 x 4 matrix of bytes, a row in each of the lanes whose numbers differ in bits 2 and 3, turned over.
+__device__ inline uint32_t turn_bytes(uint32_t word, int lane) {
+  uint32_t far = (uint32_t)__shfl_xor((int)word, 4);
+  word = __builtin_amdgcn_perm(far, word, lane & 4 ? 0x03070105u : 0x06020400u);
+  far = (uint32_t)__shfl_xor((int)word, 8);
+  return __builtin_amdgcn_perm(far, word, lane & 8 ? 0x03020706u : 0x05040100u);
+}
+
+// Queries, keys and values have workgroups of their own.  A group of lanes takes BUNDLE heads of a token, whose loads are under way together;
+// position, table row and weight serve all of them.
+template <bool BF, int BUNDLE>
 __global__ __launch_bounds__(kBlock) void turn_kernel(const TurnArgs a) {
 #pragma clang fp contract(off)     // products are rounded before they are added: keys near the edge of two codes take the same one everywhere
-  const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1), groups = kBlock >> a.lane_bits;
-  const int64_t first = (int64_t)blockIdx.x * (groups * a.rounds) + (threadIdx.x >> a.lane_bits);
+  const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1), groups = kBlock >> a.lane_bits, n = a.dim / 32;
   const bool mine = lane * 8 < a.dim;
-  for (int round = 0; round < a.rounds; ++round) {
-    const int64_t item = first + (int64_t)round * groups;
-    if (item >= a.items) return;                          // the same for all lanes of a head
-    const int64_t token = item / a.all_heads;
-    int head = (int)(item - token * a.all_heads);
-    const int kind = head < a.heads ? 0 : head < a.heads + a.pool.heads ? 1 : 2;
-    head -= kind == 0 ? 0 : kind == 1 ? a.heads : a.heads + a.pool.heads;
-    const Heads src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+  for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
+    const int kind = block < a.part[0].blocks ? 0 : block < a.part[0].blocks + a.part[1].blocks ? 1 : 2;
+    const Heads& part = a.part[kind];
+    const int64_t first = (block - (kind > 0 ? a.part[0].blocks : 0) - (kind > 1 ? a.part[1].blocks : 0)) * groups;
+    const int64_t first_token = first / part.bundles;
+    const uint32_t at_bundle = (uint32_t)(first - first_token * part.bundles) + (threadIdx.x >> a.lane_bits), skip = at_bundle / (uint32_t)part.bundles;
+    const int64_t token = first_token + skip;
+    const int head = (int)(at_bundle - skip * part.bundles) * BUNDLE;
+    if (token >= a.tokens) continue;                      // the same for all lanes of a group
 
-    Packed8 raw = {0, 0, 0, 0};
-    if (mine) raw = *reinterpret_cast<const Packed8Any*>(src.x + token * src.token + head * src.head + lane * 8);
-    float y[8];
-    unpack8<BF>(raw, y);
+    Packed8 raw[BUNDLE];
+    const uint16_t* const src = part.x + token * part.token + head * part.head + lane * 8;
+#pragma unroll
+    for (int i = 0; i < BUNDLE; ++i) {
+      raw[i] = Packed8{0, 0, 0, 0};
+      if (mine && head + i < part.heads) raw[i] = *reinterpret_cast<const Packed8Any*>(src + i * part.head);
+    }
     bool placed = true;
-    if (kind < 2) {
-      // the lane that holds the other channels of this one's pairs
-      const int half = a.rot >> 4;                        // lanes of half a turned part
-      const bool turned = lane < 2 * half;
-      float z[8];
-      if (!a.interleaved) {
-        const int other = !turned ? lane : lane < half ? lane + half : lane - half;
-        Packed8 far;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) far[i] = (uint32_t)__shfl((int)raw[i], other, lanes);
-        unpack8<BF>(far, z);
-      }
-      const uint16_t* weight = kind == 0 ? a.q_weight : a.k_weight;
-      if (weight) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += y[i] * y[i];
-        const float r = 1.f / sqrtf(group_sum(sum, lanes) / (float)a.dim + a.eps);
-        if (mine) {
-          float w[8];
-          unpack8<BF>(*reinterpret_cast<const Packed8Any*>(weight + lane * 8), w);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = y[i] * r * w[i];
-          if (!a.interleaved && turned) {
-            unpack8<BF>(*reinterpret_cast<const Packed8Any*>(weight + (lane < half ? lane + half : lane - half) * 8), w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = z[i] * r * w[i];
-          }
-        }
-      }
-      if (a.rot > 0) {
-        const int64_t at = a.positions[token];
-        placed = at >= 0 && at < a.table_rows;
-        if (placed && turned) {
-          const float* row = a.table + at * a.rot;
-          if (a.interleaved) {
-            const float4 c = *reinterpret_cast<const float4*>(row + lane * 4), s = *reinterpret_cast<const float4*>(row + a.rot / 2 + lane * 4);
-            const float cs[4] = {c.x, c.y, c.z, c.w}, sn[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float u = y[2 * i], w = y[2 * i + 1];
-              y[2 * i] = u * cs[i] - w * sn[i];
-              y[2 * i + 1] = u * sn[i] + w * cs[i];
-            }
-          } else {
-            const int i0 = (lane < half ? lane : lane - half) * 8;
-            const float sign = lane < half ? -1.f : 1.f;
-#pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-              const float4 c = *reinterpret_cast<const float4*>(row + i0 + i), s = *reinterpret_cast<const float4*>(row + a.rot / 2 + i0 + i);
-              const float cs[4] = {c.x, c.y, c.z, c.w}, sn[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-              for (int t = 0; t < 4; ++t) y[i + t] = y[i + t] * cs[t] + sign * (z[i + t] * sn[t]);
-            }
-          }
-        }
-      }
-    }
-    if (kind == 0) {
-      if (!placed) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = NAN;
-      }
-      if (mine) *reinterpret_cast<Packed8Any*>(a.out + token * a.out_token + head * a.out_head + lane * 8) = pack8<BF>(y);
-      continue;
-    }
-    if (kind == 2 && a.rot > 0) {
-      const int64_t at = a.positions[token];
+    int64_t at = 0, slot = 0;
+    if (a.rot > 0) {
+      at = a.positions[token];
       placed = at >= 0 && at < a.table_rows;
     }
-    const int64_t slot = a.slots[token];
-    uint32_t byte;
-    const uint32_t word = encode8(y, &byte);
-    if (!placed || slot < 0 || slot >= a.slots_held) continue;
-    const int n = a.dim / 32;
-    const KvToken to = kv_token(a.pool, slot >> a.pool.page_bits, head, (int)(slot & ((1 << a.pool.page_bits) - 1)));
-    if (kind == 1) {
-      if (mine) {
-        reinterpret_cast<uint32_t*>(to.keys)[lane] = word;
-        if ((lane & 3) == 0) to.key_bytes[lane >> 2] = (uint8_t)byte;
-      }
-    } else {
-      // lanes 4g + 2u + v hold channels 32g + 16u + 8v + e: a byte takes the same e from u = 0 and u = 1
-      const uint32_t far = (uint32_t)__shfl_xor((int)word, 2);
-      const bool upper = lane & 2;
-      const uint32_t low = upper ? far >> 16 : word, high = upper ? word >> 16 : far;
-      if (mine) {
-        uint8_t* at = to.values + ((lane & 1) * 8 + (upper ? 4 : 0)) * 4 * n + (lane >> 2);
+    if (kind > 0) slot = a.slots[token];
+    const int half = a.rot >> 4;                          // lanes of half a turned part
+    const bool turned = kind < 2 && placed && lane < 2 * half;
+    const int other = lane >= 2 * half ? lane : lane < half ? lane + half : lane - half;      // the lane that holds the other channels of this one's pairs
+    float c[8], s[8], w[8];
+    if (turned) {
+      const float* const row = a.table + at * a.rot + (a.interleaved ? lane * 4 : (lane < half ? lane : other) * 8);
+      *reinterpret_cast<V4*>(c) = *reinterpret_cast<const V4*>(row);
+      *reinterpret_cast<V4*>(s) = *reinterpret_cast<const V4*>(row + a.rot / 2);
+      if (!a.interleaved) {
+        *reinterpret_cast<V4*>(c + 4) = *reinterpret_cast<const V4*>(row + 4);
+        *reinterpret_cast<V4*>(s + 4) = *reinterpret_cast<const V4*>(row + a.rot / 2 + 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) at[e * 4 * n] = (uint8_t)((low >> (4 * e) & 15u) | (high >> (4 * e) & 15u) << 4);
-        if ((lane & 3) == 0) to.value_bytes[lane >> 2] = (uint8_t)byte;
+        for (int i = 0; i < 8; ++i) s[i] = lane < half ? -s[i] : s[i];
       }
+    }
+    if (part.weight && mine) unpack8<BF>(*reinterpret_cast<const Packed8Any*>(part.weight + lane * 8), w);
+
+#pragma unroll
+    for (int i = 0; i < BUNDLE; ++i) {
+      if (head + i >= part.heads) break;
+      float y[8];
+      unpack8<BF>(raw[i], y);
+      if (part.weight) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
+        const float r = 1.f / sqrtf(group_sum(sum, lanes) / (float)a.dim + a.eps);
+        if (mine) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = y[e] * r * w[e];
+        }
+      }
+      if (kind < 2 && a.rot > 0) {
+        if (a.interleaved) {
+          if (turned) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float u = y[2 * e], v = y[2 * e + 1];
+              y[2 * e] = u * c[e] - v * s[e];
+              y[2 * e + 1] = u * s[e] + v * c[e];
+            }
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float z = __shfl(y[e], other, lanes);
+            if (turned) y[e] = y[e] * c[e] + z * s[e];
+          }
+        }
+      }
+      if (kind == 0) {
+        if (!placed) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = NAN;
+        }
+        if (mine) *reinterpret_cast<Packed8Any*>(a.out + token * a.out_token + (head + i) * a.out_head + lane * 8) = pack8<BF>(y);
+        continue;
+      }
+      uint32_t byte;
+      uint32_t word = encode8(y, &byte);
+      if (!placed || slot < 0 || slot >= a.slots_held) continue;
+      const KvToken to = kv_token(a.pool, slot >> a.pool.page_bits, head + i, (int)(slot & ((1 << a.pool.page_bits) - 1)));
+      if (kind == 1) {
+        if (mine) {
+          reinterpret_cast<uint32_t*>(to.keys)[lane] = word;
+          if ((lane & 3) == 0) to.key_bytes[lane >> 2] = (uint8_t)byte;
+        }
+        continue;
+      }
+      word = pair_values(word, lane & 2);
+      uint8_t* at_m = to.values + ((lane & 1) * 8 + (lane & 2) * 2) * 4 * n;
+      if (n == 4) {                                       // a whole word a lane
+        *reinterpret_cast<uint32_t*>(at_m + (lane >> 2) * 16) = turn_bytes(word, lane);
+      } else if (mine) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) at_m[e * 4 * n + (lane >> 2)] = (uint8_t)(word >> (8 * e));
+      }
+      if (mine && (lane & 3) == 0) to.value_bytes[lane >> 2] = (uint8_t)byte;
     }
   }
 }
@@ -186,12 +203,12 @@ __global__ __launch_bounds__(kBlock) void turn_kernel(const TurnArgs a) {
 struct ReadArgs {
   KvPool pool;
   const int32_t* slots;
-  int64_t items, slots_held;
+  int64_t tokens, slots_held, blocks;
   uint16_t* k;
   int64_t k_token, k_head;
   uint16_t* v;
   int64_t v_token, v_head;
-  int32_t lane_bits;
+  int32_t lane_bits, bundles;
 };
 
 // Two 4-bit codes as 16-bit values, times 2^(b - 127).
@@ -212,28 +229,49 @@ __device__ inline Packed8 decode8(uint32_t word, uint32_t byte) {
   return {decode2<BF, 0>(word, unit), decode2<BF, 1>(word, unit), decode2<BF, 2>(word, unit), decode2<BF, 3>(word, unit)};
 }
 
-template <bool BF>
+template <bool BF, int BUNDLE>
 __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
-  const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1), groups = kBlock >> a.lane_bits;
-  if (lane * 8 >= a.pool.dim) return;
-  for (int64_t item = (int64_t)blockIdx.x * groups + (threadIdx.x >> a.lane_bits); item < a.items; item += (int64_t)gridDim.x * groups) {
-    const int64_t token = item / a.pool.heads;
-    const int head = (int)(item - token * a.pool.heads), n = a.pool.dim / 32;
+  const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1), groups = kBlock >> a.lane_bits, n = a.pool.dim / 32;
+  const bool mine = lane * 8 < a.pool.dim;
+  for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
+    const int64_t first = block * groups, first_token = first / a.bundles;
+    const uint32_t at_bundle = (uint32_t)(first - first_token * a.bundles) + (threadIdx.x >> a.lane_bits), skip = at_bundle / (uint32_t)a.bundles;
+    const int64_t token = first_token + skip;
+    const int head = (int)(at_bundle - skip * a.bundles) * BUNDLE;
+    if (token >= a.tokens) continue;
     const int64_t slot = a.slots[token];
-    Packed8 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-    if (slot >= 0 && slot < a.slots_held) {
-      const KvToken from = kv_token(a.pool, slot >> a.pool.page_bits, head, (int)(slot & ((1 << a.pool.page_bits) - 1)));
-      if (a.k) k = decode8<BF>(reinterpret_cast<const uint32_t*>(from.keys)[lane], from.key_bytes[lane >> 2]);
-      if (a.v) {
-        const uint8_t* at = from.values + (lane & 1) * 8 * 4 * n + (lane >> 2);
-        uint32_t word = 0;
-  #pragma unroll
-        for (int e = 0; e < 8; ++e) word |= (uint32_t)(at[e * 4 * n] >> (lane & 2 ? 4 : 0) & 15) << (4 * e);
-        v = decode8<BF>(word, from.value_bytes[lane >> 2]);
+    const bool there = slot >= 0 && slot < a.slots_held && mine;
+    uint32_t key[BUNDLE], value[BUNDLE], key_byte[BUNDLE], value_byte[BUNDLE];
+#pragma unroll
+    for (int i = 0; i < BUNDLE; ++i) {
+      key[i] = value[i] = key_byte[i] = value_byte[i] = 0;
+      if (there && head + i < a.pool.heads) {
+        const KvToken from = kv_token(a.pool, slot >> a.pool.page_bits, head + i, (int)(slot & ((1 << a.pool.page_bits) - 1)));
+        if (a.k) {
+          key[i] = reinterpret_cast<const uint32_t*>(from.keys)[lane];
+          key_byte[i] = from.key_bytes[lane >> 2];
+        }
+        if (a.v) {
+          const uint8_t* const at_m = from.values + ((lane & 1) * 8 + (lane & 2) * 2) * 4 * n;
+          if (n == 4) {
+            value[i] = *reinterpret_cast<const uint32_t*>(at_m + (lane >> 2) * 16);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) value[i] |= (uint32_t)at_m[e * 4 * n + (lane >> 2)] << (8 * e);
+          }
+          value_byte[i] = from.value_bytes[lane >> 2];
+        }
       }
     }
-    if (a.k) *reinterpret_cast<Packed8Any*>(a.k + token * a.k_token + head * a.k_head + lane * 8) = k;
-    if (a.v) *reinterpret_cast<Packed8Any*>(a.v + token * a.v_token + head * a.v_head + lane * 8) = v;
+#pragma unroll
+    for (int i = 0; i < BUNDLE; ++i) {
+      if (head + i >= a.pool.heads) break;
+      if (a.k && mine) *reinterpret_cast<Packed8Any*>(a.k + token * a.k_token + (head + i) * a.k_head + lane * 8) = decode8<BF>(key[i], key_byte[i]);
+      if (a.v) {
+        const uint32_t word = unpair_values(n == 4 ? turn_bytes(value[i], lane) : value[i], lane & 2);
+        if (mine) *reinterpret_cast<Packed8Any*>(a.v + token * a.v_token + (head + i) * a.v_head + lane * 8) = decode8<BF>(word, value_byte[i]);
+      }
+    }
   }
 }
 
@@ -302,17 +340,27 @@ int launched() {
   return e == hipSuccess ? MACKO_OK : hip_fail(e);
 }
 
-int launch_turn(TurnArgs& a, int64_t tokens, int type, hipStream_t stream) {
+// Heads that a group of lanes takes together: 4 where that leaves enough groups to fill the device.
+constexpr int kBundle = 4;
+bool bundled(int64_t items, int lane_bits) { return items >> (8 - lane_bits) >= (int64_t)device_cu_count() * 16; }
+
+int launch_turn(TurnArgs& a, int type, hipStream_t stream) {
   a.lane_bits = lane_bits_of(a.dim);
-  a.items = tokens * a.all_heads;
-  const int64_t groups = kBlock >> a.lane_bits, target = (int64_t)device_cu_count() * 16;
-  int64_t rounds = std::min<int64_t>(4, std::max<int64_t>(1, a.items / (groups * target)));
-  rounds = std::max(rounds, (a.items + groups * kMostBlocks - 1) / (groups * kMostBlocks));
-  if (rounds > INT32_MAX / kBlock) return MACKO_E_UNSUPPORTED;
-  a.rounds = (int32_t)rounds;
-  const int64_t blocks = (a.items + groups * rounds - 1) / (groups * rounds);
-  if (type == MACKO_BF16) hipLaunchKernelGGL(turn_kernel<true>, dim3((unsigned)blocks), dim3(kBlock), 0, stream, a);
-  else hipLaunchKernelGGL(turn_kernel<false>, dim3((unsigned)blocks), dim3(kBlock), 0, stream, a);
+  const int64_t groups = kBlock >> a.lane_bits;
+  const int all = a.part[0].heads + a.part[1].heads + a.part[2].heads, bundle = bundled(a.tokens * all, a.lane_bits) ? kBundle : 1;
+  for (Heads& h : a.part) {
+    h.bundles = std::max(1, (h.heads + bundle - 1) / bundle);
+    h.blocks = h.heads ? (a.tokens * h.bundles + groups - 1) / groups : 0;
+    a.blocks += h.blocks;
+  }
+  const dim3 grid((unsigned)std::min(a.blocks, kMostBlocks)), block(kBlock);
+  if (type == MACKO_BF16) {
+    if (bundle > 1) hipLaunchKernelGGL((turn_kernel<true, kBundle>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((turn_kernel<true, 1>), grid, block, 0, stream, a);
+  } else {
+    if (bundle > 1) hipLaunchKernelGGL((turn_kernel<false, kBundle>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((turn_kernel<false, 1>), grid, block, 0, stream, a);
+  }
   return launched();
 }
 
@@ -381,15 +429,14 @@ int macko_rotate(int64_t tokens, int heads, int head_dim, int type, const void* 
   if (tokens > INT32_MAX || heads > 65536) return MACKO_E_UNSUPPORTED;
   if (!heads_fine(x_dev, x_token, x_head) || !heads_fine(out_dev, out_token, out_head) || !aligned_to(weight_dev, 2)) return MACKO_E_INVALID_ARG;
   TurnArgs a{};
-  a.q = {static_cast<const uint16_t*>(x_dev), x_token, x_head};
+  a.part[0] = Heads{static_cast<const uint16_t*>(x_dev), x_token, x_head, static_cast<const uint16_t*>(weight_dev), heads, 0, 0};
   a.out = static_cast<uint16_t*>(out_dev);
   a.out_token = out_token;
   a.out_head = out_head;
-  a.q_weight = static_cast<const uint16_t*>(weight_dev);
-  a.heads = a.all_heads = heads;
+  a.tokens = tokens;
   a.dim = head_dim;
   set_rotation(a, *rotation);
-  return launch_turn(a, tokens, type, static_cast<hipStream_t>(stream));
+  return launch_turn(a, type, static_cast<hipStream_t>(stream));
 }
 
 int macko_kv_append(const macko_kv_cache_t* cache, const macko_kv_append_args_t* g, void* stream) {
@@ -404,22 +451,19 @@ int macko_kv_append(const macko_kv_cache_t* cache, const macko_kv_append_args_t*
     return MACKO_E_INVALID_ARG;
   if (g->heads > 0 && (!heads_fine(g->q_dev, g->q_token, g->q_head) || !heads_fine(g->q_out_dev, g->q_out_token, g->q_out_head))) return MACKO_E_INVALID_ARG;
   TurnArgs a{};
-  a.q = {static_cast<const uint16_t*>(g->q_dev), g->q_token, g->q_head};
-  a.k = {static_cast<const uint16_t*>(g->k_dev), g->k_token, g->k_head};
-  a.v = {static_cast<const uint16_t*>(g->v_dev), g->v_token, g->v_head};
+  a.part[0] = Heads{static_cast<const uint16_t*>(g->q_dev), g->q_token, g->q_head, static_cast<const uint16_t*>(g->q_weight_dev), g->heads, 0, 0};
+  a.part[1] = Heads{static_cast<const uint16_t*>(g->k_dev), g->k_token, g->k_head, static_cast<const uint16_t*>(g->k_weight_dev), pool.heads, 0, 0};
+  a.part[2] = Heads{static_cast<const uint16_t*>(g->v_dev), g->v_token, g->v_head, nullptr, pool.heads, 0, 0};
   a.out = static_cast<uint16_t*>(g->q_out_dev);
   a.out_token = g->q_out_token;
   a.out_head = g->q_out_head;
-  a.q_weight = static_cast<const uint16_t*>(g->q_weight_dev);
-  a.k_weight = static_cast<const uint16_t*>(g->k_weight_dev);
   a.slots = g->slots_dev;
   a.pool = pool;
   a.slots_held = pool.pages << pool.page_bits;
-  a.heads = g->heads;
-  a.all_heads = g->heads + 2 * pool.heads;
+  a.tokens = g->tokens;
   a.dim = pool.dim;
   set_rotation(a, g->rotation);
-  return launch_turn(a, g->tokens, g->type, static_cast<hipStream_t>(stream));
+  return launch_turn(a, g->type, static_cast<hipStream_t>(stream));
 }
 
 int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const int32_t* slots_dev, int type, void* k_out_dev, int64_t k_token, int64_t k_head,
@@ -431,13 +475,18 @@ int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const int32_t* 
   if (tokens > INT32_MAX) return MACKO_E_UNSUPPORTED;
   if (!slots_dev || !aligned_to(slots_dev, 4) || (k_out_dev && !heads_fine(k_out_dev, k_token, k_head)) || (v_out_dev && !heads_fine(v_out_dev, v_token, v_head)))
     return MACKO_E_INVALID_ARG;
-  const int bits = lane_bits_of(pool.dim), groups = kBlock >> bits;
-  const ReadArgs a{pool, slots_dev, tokens * pool.heads, pool.pages << pool.page_bits, static_cast<uint16_t*>(k_out_dev), k_token, k_head,
-                   static_cast<uint16_t*>(v_out_dev), v_token, v_head, bits};
-  const int64_t blocks = std::min(kMostBlocks, (a.items + groups - 1) / groups);
+  const int bits = lane_bits_of(pool.dim), groups = kBlock >> bits, bundle = bundled(tokens * pool.heads, bits) ? kBundle : 1, bundles = (pool.heads + bundle - 1) / bundle;
+  const ReadArgs a{pool, slots_dev, tokens, pool.pages << pool.page_bits, (tokens * bundles + groups - 1) / groups, static_cast<uint16_t*>(k_out_dev), k_token, k_head,
+                   static_cast<uint16_t*>(v_out_dev), v_token, v_head, bits, bundles};
+  const dim3 grid((unsigned)std::min(a.blocks, kMostBlocks)), block(kBlock);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (type == MACKO_BF16) hipLaunchKernelGGL(read_kernel<true>, dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
-  else hipLaunchKernelGGL(read_kernel<false>, dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
+  if (type == MACKO_BF16) {
+    if (bundle > 1) hipLaunchKernelGGL((read_kernel<true, kBundle>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((read_kernel<true, 1>), grid, block, 0, s, a);
+  } else {
+    if (bundle > 1) hipLaunchKernelGGL((read_kernel<false, kBundle>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((read_kernel<false, 1>), grid, block, 0, s, a);
+  }
   return launched();
 }
 
