@@ -63,11 +63,19 @@ __device__ inline void unpack8(Packed8 p, float* x) {
   }
 }
 template <bool BF>
+__device__ inline uint32_t pack2(float x, float y) {
+  if (BF) {
+    typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+    const B2 p = {(__bf16)x, (__bf16)y};
+    return __builtin_bit_cast(uint32_t, p);
+  }
+  typedef _Float16 H2 __attribute__((ext_vector_type(2)));
+  const H2 p = {(_Float16)x, (_Float16)y};
+  return __builtin_bit_cast(uint32_t, p);
+}
+template <bool BF>
 __device__ inline Packed8 pack8(const float* x) {
-  Packed8 p;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) p[i] = to_bits<BF>(x[2 * i]) | to_bits<BF>(x[2 * i + 1]) << 16;
-  return p;
+  return {pack2<BF>(x[0], x[1]), pack2<BF>(x[2], x[3]), pack2<BF>(x[4], x[5]), pack2<BF>(x[6], x[7])};
 }
 
 struct KvAttention {

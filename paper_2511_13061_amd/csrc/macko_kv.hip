@@ -5,6 +5,7 @@
 // group of 4 to 32 lanes with 8 channels each takes it in one 16-byte load a lane; what a head needs of other lanes (the sum of a norm, the
 // other half of a pair, a group's largest magnitude) goes through lane shuffles, so that nothing is read twice and in-place calls are safe.
 #include <cmath>
+#include <type_traits>
 
 #include "macko_kv.h"
 
@@ -23,6 +24,13 @@ struct Heads {
   int32_t bundles;           // of a token: heads that a group of lanes takes together
   int64_t blocks;            // that the launch has for these heads
 };
+// Results of a large call leave the caches to others: they are larger than those, and what is read stays longer.
+template <bool STREAM>
+__device__ inline void put8(uint16_t* to, Packed8 x) {
+  if (STREAM) __builtin_nontemporal_store((Packed8Any)x, reinterpret_cast<Packed8Any*>(to));
+  else *reinterpret_cast<Packed8Any*>(to) = x;
+}
+
 struct TurnArgs {
   Heads part[3];             // queries, keys, values
   uint16_t* out;
@@ -38,8 +46,20 @@ struct TurnArgs {
   float eps;
 };
 
+template <int CTRL>
+__device__ inline uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;      // quad_perm [1,0,3,2] and [2,3,0,1], row_half_mirror, row_mirror
+
+// The sum over a group of 4 to 32 lanes, in all of them.
 __device__ inline float group_sum(float x, int lanes) {
-  for (int m = 1; m < lanes; m <<= 1) x += __shfl_xor(x, m);
+  auto with = [](float y, uint32_t far) { return y + __builtin_bit_cast(float, far); };
+  x = with(x, dpp<kSwap1>(__builtin_bit_cast(uint32_t, x)));
+  x = with(x, dpp<kSwap2>(__builtin_bit_cast(uint32_t, x)));
+  if (lanes > 4) x = with(x, dpp<kMirror8>(__builtin_bit_cast(uint32_t, x)));      // quads hold one sum each: any lane of the other will do
+  if (lanes > 8) x = with(x, dpp<kMirror16>(__builtin_bit_cast(uint32_t, x)));
+  if (lanes > 16) x += __shfl_xor(x, 16);
   return x;
 }
 
@@ -48,8 +68,8 @@ __device__ inline uint32_t encode8(const float* y, uint32_t* byte) {
   uint32_t bits = 0;                                     // magnitudes are ordered as their bits are, infinities and NaN above all
 #pragma unroll
   for (int i = 0; i < 8; ++i) bits = max(bits, __builtin_bit_cast(uint32_t, y[i]) & 0x7FFFFFFFu);
-  bits = max(bits, (uint32_t)__shfl_xor((int)bits, 1));
-  bits = max(bits, (uint32_t)__shfl_xor((int)bits, 2));
+  bits = max(bits, dpp<kSwap1>(bits));
+  bits = max(bits, dpp<kSwap2>(bits));
   // the exponent of most / 7, rounded up: 7 = 1.75 * 2^2, and a mantissa above 1.75 carries
   const uint32_t e = (bits + 0x1FFFFFu) >> 23;
   const uint32_t b = bits >= 0x7F800000u ? 255u : e > 2u ? e - 2u : 0u;
@@ -66,7 +86,7 @@ __device__ inline uint32_t encode8(const float* y, uint32_t* byte) {
 // Lanes 4g + 2u + v hold the codes of channels 32g + 16u + 8v + e as keys are stored, 8 of them in a word; a byte of the values' layout takes
 // the same e from u = 0 and u = 1.  The word of lane 4g + 2u + v here: bytes m = 8v + 4u + (0 .. 3) of group g.  And back.
 __device__ inline uint32_t pair_values(uint32_t word, bool upper) {
-  const uint32_t far = (uint32_t)__shfl_xor((int)word, 2);
+  const uint32_t far = dpp<kSwap2>(word);
   const uint32_t low = upper ? far >> 16 : word & 0xFFFFu, high = upper ? word >> 16 : far & 0xFFFFu;
   // 4 codes to the low halves of 4 bytes, 4 to the high ones
   const uint32_t a = (low | low << 8) & 0x00FF00FFu, b = (high | high << 8) & 0x00FF00FFu;
@@ -76,7 +96,7 @@ __device__ inline uint32_t unpair_values(uint32_t word, bool upper) {
   uint32_t a = word & 0x0F0F0F0Fu, b = word >> 4 & 0x0F0F0F0Fu;
   a = (a | a >> 4) & 0x00FF00FFu, b = (b | b >> 4) & 0x00FF00FFu;
   a = (a | a >> 8) & 0xFFFFu, b = (b | b >> 8) & 0xFFFFu;
-  const uint32_t give = upper ? a : b, far = (uint32_t)__shfl_xor((int)give, 2);
+  const uint32_t give = upper ? a : b, far = dpp<kSwap2>(give);
   return upper ? far | b << 16 : a | far << 16;
 }
 // A 4 x 4 matrix of bytes, a row in each of the lanes whose numbers differ in bits 2 and 3, turned over.
@@ -121,7 +141,7 @@ __global__ __launch_bounds__(kBlock) void turn_kernel(const TurnArgs a) {
     const int half = a.rot >> 4;                          // lanes of half a turned part
     const bool turned = kind < 2 && placed && lane < 2 * half;
     const int other = lane >= 2 * half ? lane : lane < half ? lane + half : lane - half;      // the lane that holds the other channels of this one's pairs
-    float c[8], s[8], w[8];
+    float c[8], s[8], w[8] = {};
     if (turned) {
       const float* const row = a.table + at * a.rot + (a.interleaved ? lane * 4 : (lane < half ? lane : other) * 8);
       *reinterpret_cast<V4*>(c) = *reinterpret_cast<const V4*>(row);
@@ -135,67 +155,85 @@ __global__ __launch_bounds__(kBlock) void turn_kernel(const TurnArgs a) {
     }
     if (part.weight && mine) unpack8<BF>(*reinterpret_cast<const Packed8Any*>(part.weight + lane * 8), w);
 
+    // A head of the bundle, normalised and turned; what varies by call and not by lane is settled outside the loops.
+    auto finish = [&](Packed8 x, float* y, auto normed, auto interleaved) {
+      unpack8<BF>(x, y);
+      if constexpr (normed) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(y[e], y[e], sum);
+        const float r = rsqrtf(group_sum(sum, lanes) / (float)a.dim + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = y[e] * r * w[e];
+      }
+      if (a.rot == 0) return;
+      if constexpr (interleaved) {
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float u = y[2 * e], v = y[2 * e + 1];
+            y[2 * e] = u * c[e] - v * s[e];
+            y[2 * e + 1] = u * s[e] + v * c[e];
+          }
+        }
+      } else {
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other, lanes);
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = y[e] * c[e] + z[e] * s[e];
+        }
+      }
+    };
+    const bool stored = placed && slot >= 0 && slot < a.slots_held;
+    const KvToken to = kv_token(a.pool, kind > 0 && stored ? slot >> a.pool.page_bits : 0, head, kind > 0 && stored ? (int)(slot & ((1 << a.pool.page_bits) - 1)) : 0);
+    const int64_t piece = kv_piece_bytes(int64_t{1} << a.pool.page_bits, a.dim);
+    auto heads = [&](auto normed, auto interleaved) {
+      uint16_t* const out = a.out + token * a.out_token + head * a.out_head + lane * 8;
+#pragma unroll
+      for (int i = 0; i < BUNDLE; ++i) {
+        if (head + i >= part.heads) break;
+        float y[8];
+        finish(raw[i], y, normed, interleaved);
+        if (kind == 0) {
+          Packed8 x = pack8<BF>(y);
+          if (__any(!placed) && !placed) x = Packed8{0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};      // NaN in both types
+          if (mine) put8<(BUNDLE > 1)>(out + i * a.out_head, x);
+        } else {
+          uint32_t byte;
+          const uint32_t word = encode8(y, &byte);
+          if (stored && mine) {
+            reinterpret_cast<uint32_t*>(to.keys + i * piece)[lane] = word;
+            if ((lane & 3) == 0) to.key_bytes[i * piece + (lane >> 2)] = (uint8_t)byte;
+          }
+        }
+      }
+    };
+    typedef std::integral_constant<bool, true> Yes;
+    typedef std::integral_constant<bool, false> No;
+    if (kind < 2) {
+      if (part.weight) a.interleaved ? heads(Yes{}, Yes{}) : heads(Yes{}, No{});
+      else a.interleaved ? heads(No{}, Yes{}) : heads(No{}, No{});
+      continue;
+    }
+    uint8_t* const at_m = to.values + ((lane & 1) * 8 + (lane & 2) * 2) * 4 * n + (n == 4 ? (lane >> 2) * 16 : lane >> 2);
 #pragma unroll
     for (int i = 0; i < BUNDLE; ++i) {
       if (head + i >= part.heads) break;
       float y[8];
       unpack8<BF>(raw[i], y);
-      if (part.weight) {
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
-        const float r = 1.f / sqrtf(group_sum(sum, lanes) / (float)a.dim + a.eps);
-        if (mine) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = y[e] * r * w[e];
-        }
-      }
-      if (kind < 2 && a.rot > 0) {
-        if (a.interleaved) {
-          if (turned) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float u = y[2 * e], v = y[2 * e + 1];
-              y[2 * e] = u * c[e] - v * s[e];
-              y[2 * e + 1] = u * s[e] + v * c[e];
-            }
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float z = __shfl(y[e], other, lanes);
-            if (turned) y[e] = y[e] * c[e] + z * s[e];
-          }
-        }
-      }
-      if (kind == 0) {
-        if (!placed) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = NAN;
-        }
-        if (mine) *reinterpret_cast<Packed8Any*>(a.out + token * a.out_token + (head + i) * a.out_head + lane * 8) = pack8<BF>(y);
-        continue;
-      }
       uint32_t byte;
-      uint32_t word = encode8(y, &byte);
-      if (!placed || slot < 0 || slot >= a.slots_held) continue;
-      const KvToken to = kv_token(a.pool, slot >> a.pool.page_bits, head + i, (int)(slot & ((1 << a.pool.page_bits) - 1)));
-      if (kind == 1) {
-        if (mine) {
-          reinterpret_cast<uint32_t*>(to.keys)[lane] = word;
-          if ((lane & 3) == 0) to.key_bytes[lane >> 2] = (uint8_t)byte;
-        }
-        continue;
-      }
-      word = pair_values(word, lane & 2);
-      uint8_t* at_m = to.values + ((lane & 1) * 8 + (lane & 2) * 2) * 4 * n;
+      uint32_t word = pair_values(encode8(y, &byte), lane & 2);
+      if (n == 4) word = turn_bytes(word, lane);
+      if (!stored || !mine) continue;
       if (n == 4) {                                       // a whole word a lane
-        *reinterpret_cast<uint32_t*>(at_m + (lane >> 2) * 16) = turn_bytes(word, lane);
-      } else if (mine) {
+        *reinterpret_cast<uint32_t*>(at_m + i * piece) = word;
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) at_m[e * 4 * n + (lane >> 2)] = (uint8_t)(word >> (8 * e));
+        for (int e = 0; e < 4; ++e) at_m[i * piece + e * 4 * n] = (uint8_t)(word >> (8 * e));
       }
-      if (mine && (lane & 3) == 0) to.value_bytes[lane >> 2] = (uint8_t)byte;
+      if ((lane & 3) == 0) to.value_bytes[i * piece + (lane >> 2)] = (uint8_t)byte;
     }
   }
 }
@@ -242,34 +280,35 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
     const int64_t slot = a.slots[token];
     const bool there = slot >= 0 && slot < a.slots_held && mine;
     uint32_t key[BUNDLE], value[BUNDLE], key_byte[BUNDLE], value_byte[BUNDLE];
+    const KvToken from = kv_token(a.pool, there ? slot >> a.pool.page_bits : 0, head, there ? (int)(slot & ((1 << a.pool.page_bits) - 1)) : 0);
+    const uint8_t* const at_m = from.values + ((lane & 1) * 8 + (lane & 2) * 2) * 4 * n + (n == 4 ? (lane >> 2) * 16 : lane >> 2);
+    const int64_t piece = kv_piece_bytes(int64_t{1} << a.pool.page_bits, a.pool.dim);
 #pragma unroll
     for (int i = 0; i < BUNDLE; ++i) {
       key[i] = value[i] = key_byte[i] = value_byte[i] = 0;
       if (there && head + i < a.pool.heads) {
-        const KvToken from = kv_token(a.pool, slot >> a.pool.page_bits, head + i, (int)(slot & ((1 << a.pool.page_bits) - 1)));
         if (a.k) {
-          key[i] = reinterpret_cast<const uint32_t*>(from.keys)[lane];
-          key_byte[i] = from.key_bytes[lane >> 2];
+          key[i] = reinterpret_cast<const uint32_t*>(from.keys + i * piece)[lane];
+          key_byte[i] = from.key_bytes[i * piece + (lane >> 2)];
         }
         if (a.v) {
-          const uint8_t* const at_m = from.values + ((lane & 1) * 8 + (lane & 2) * 2) * 4 * n;
           if (n == 4) {
-            value[i] = *reinterpret_cast<const uint32_t*>(at_m + (lane >> 2) * 16);
+            value[i] = *reinterpret_cast<const uint32_t*>(at_m + i * piece);
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) value[i] |= (uint32_t)at_m[e * 4 * n + (lane >> 2)] << (8 * e);
+            for (int e = 0; e < 4; ++e) value[i] |= (uint32_t)at_m[i * piece + e * 4 * n] << (8 * e);
           }
-          value_byte[i] = from.value_bytes[lane >> 2];
+          value_byte[i] = from.value_bytes[i * piece + (lane >> 2)];
         }
       }
     }
 #pragma unroll
     for (int i = 0; i < BUNDLE; ++i) {
       if (head + i >= a.pool.heads) break;
-      if (a.k && mine) *reinterpret_cast<Packed8Any*>(a.k + token * a.k_token + (head + i) * a.k_head + lane * 8) = decode8<BF>(key[i], key_byte[i]);
+      if (a.k && mine) put8<(BUNDLE > 1)>(a.k + token * a.k_token + (head + i) * a.k_head + lane * 8, decode8<BF>(key[i], key_byte[i]));
       if (a.v) {
         const uint32_t word = unpair_values(n == 4 ? turn_bytes(value[i], lane) : value[i], lane & 2);
-        if (mine) *reinterpret_cast<Packed8Any*>(a.v + token * a.v_token + (head + i) * a.v_head + lane * 8) = decode8<BF>(word, value_byte[i]);
+        if (mine) put8<(BUNDLE > 1)>(a.v + token * a.v_token + (head + i) * a.v_head + lane * 8, decode8<BF>(word, value_byte[i]));
       }
     }
   }
