@@ -11,78 +11,10 @@
 //            The lanes of S^T that hold a token's weights are those that P^T needs: nothing moves between lanes.
 // The four wavefronts of a workgroup take turns along the tokens and join their sums in LDS; long sequences are split over workgroups
 // too, whose unnormalised sums a second kernel joins.
-#include "macko_kv.h"
+#include "macko_kv_attention.h"
 
 namespace macko {
 namespace {
-
-typedef int V8i __attribute__((ext_vector_type(8)));
-typedef int V4i __attribute__((ext_vector_type(4)));
-typedef float V4f __attribute__((ext_vector_type(4)));
-typedef __bf16 B2 __attribute__((ext_vector_type(2)));
-typedef __bf16 B8 __attribute__((ext_vector_type(8)));
-
-constexpr int kWaves = 4, kTile = 32, kMostSplits = 256;
-constexpr int kMostTokens = 1 << 30;                  // of a sequence: sums of a length and a launch's steps stay in 31 bits
-constexpr float kLift = 8.f;       // how far, in powers of two, a score may pass the running maximum before that moves
-
-struct Grid {
-  int32_t row_blocks, splits;      // of a sequence's rows and of its tokens, at most
-  int32_t ordered;                 // long sequences first
-  int64_t chunk;                   // tokens of a split, at least; a multiple of kWaves * kTile
-  float* parts;                    // [tokens * heads][splits][D], then [tokens * heads][splits][2]: maximum and sum
-};
-
-struct Launch {
-  KvAttention a;
-  Grid g;
-};
-typedef const __attribute__((address_space(4))) Launch* LaunchPtr;
-
-struct Sequence {
-  int length, first, queries, rows;
-};
-__device__ inline Sequence sequence_of(const KvAttention& a, int b) {
-  Sequence s;
-  s.length = min(max(0, a.lengths[b]), kMostTokens);
-  s.first = a.start ? min(max(a.start[b], 0), (int)a.tokens) : b;
-  s.queries = a.start ? min(max(a.start[b + 1], s.first), (int)a.tokens) - s.first : 1;
-  s.rows = s.queries * a.shared;
-  return s;
-}
-
-// The tokens that the rows first_row .. of a block see, and how they are split.
-struct Span {
-  int lo, hi, chunk, used;         // lo: a multiple of 16
-  int all_lo, all_hi;              // every row of the block sees [all_lo, all_hi)
-};
-__device__ inline Span span_of(const KvAttention& a, const Grid& g, const Sequence& s, int first_row, int rows) {
-  Span p;
-  const int qa = first_row / a.shared, qb = min(first_row + rows - 1, s.rows - 1) / a.shared, offset = s.length - s.queries;
-  p.hi = min(max(offset + qb + 1, 0), s.length);
-  p.all_hi = min(max(offset + qa + 1, 0), s.length);
-  const int lo = a.window ? max(offset + qa - a.window + 1, 0) : 0;
-  p.all_lo = a.window ? max(offset + qb - a.window + 1, 0) : 0;
-  p.lo = min(lo, p.hi) & ~15;
-  const int range = max(p.hi - p.lo, 0), unit = kWaves * kTile;
-  p.chunk = max((int)g.chunk, (range + g.splits * unit - 1) / (g.splits * unit) * unit);
-  p.used = max(1, (range + p.chunk - 1) / p.chunk);
-  return p;
-}
-
-__device__ inline int later(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
-// The sequence that is n-th by length, longest first (at most 64 of them): workgroups start in this order, and the last ones to end are short.
-__device__ inline int nth_longest(const KvAttention& a, int n, int lane) {
-  const int key = lane < a.batch ? min(max(a.lengths[lane], 0), (1 << 25) - 1) * 64 + 63 - lane : -1;
-  int longer = 0;
-#pragma unroll
-  for (int m = 0; m < 64; ++m) longer += __builtin_amdgcn_readlane(key, m) > key;
-  return __builtin_ctzll(__ballot(longer == n && lane < a.batch));
-}
 
 // What a wavefront holds of 32 tokens: two blocks of 16.
 template <int NG>
@@ -92,21 +24,6 @@ struct Tile {
   int key_byte[2][NK];
   uint32_t value[2][NG], value_byte[2][NG];      // [token of 4][g] bytes
 };
-
-template <int BYTE>
-__device__ inline B2 decode_pair(uint32_t word, uint32_t bytes, int at) {
-  // the conversion looks at the exponent field of its scale alone
-  const uint32_t unit = at == 0 ? bytes << 23 : at == 1 ? bytes << 15 : at == 2 ? bytes << 7 : bytes >> 1;
-  return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, __builtin_bit_cast(float, unit), BYTE);
-}
-__device__ inline B2 decode_at(uint32_t word, uint32_t bytes, int at) {
-  switch (at) {
-    case 0: return decode_pair<0>(word, bytes, 0);
-    case 1: return decode_pair<1>(word, bytes, 1);
-    case 2: return decode_pair<2>(word, bytes, 2);
-    default: return decode_pair<3>(word, bytes, 3);
-  }
-}
 
 // Wavefronts on a SIMD that the registers are to leave room for.
 constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? (ng <= 4 ? 2 : 1) : ng == 1 ? 4 : ng <= 4 ? 3 : 1; }
@@ -137,11 +54,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
   for (int first_row = (int)(rest % g.row_blocks) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
-    const Span span = span_of(a, g, seq, first_row, R);
+    const Span span = span_of(a, g, seq, first_row);
     if (split >= span.used) continue;
     // What follows from the lane is worked out here and again behind the steps (later(...)): kept from outside the loop it would hold registers.
     const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4;
-    const int begin = span.lo + split * span.chunk, end = min(span.hi, begin + span.chunk);
+    const int begin = span.lo + split * span.chunk, end = span.hi - begin > span.chunk ? begin + span.chunk : span.hi;
 
     bool bad = end > begin && (a.table_width == 0 || a.pool.pages == 0);     // a page that is needed is missing
     const int last_block = (end - 1) >> 4;
@@ -205,53 +122,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       const bool there = row < seq.rows;
       place[rt] = there ? seq.length - seq.queries + query : -1;
       const uint16_t* src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        float x[2][16];
-        uint32_t top[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {                     // a lane's channels of the operand: 16 in each half of 128
-          const int channel = kk * 128 + u * 64 + j * 16;
-          Packed8 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-          if (there && channel < D) {
-            lo = *reinterpret_cast<const Packed8Any*>(src + channel);
-            hi = *reinterpret_cast<const Packed8Any*>(src + channel + 8);
-          }
-          unpack8<BF>(lo, x[u]);
-          unpack8<BF>(hi, x[u] + 8);
-          uint32_t most = 0;                              // magnitudes are ordered as their bits are, infinities and NaN above all
-#pragma unroll
-          for (int i = 0; i < 16; ++i) most = max(most, __builtin_bit_cast(uint32_t, x[u][i]) & 0x7FFFFFFFu);
-          most = max(most, (uint32_t)__shfl_xor((int)most, 16));      // two lanes share a group
-          top[u] = max(most >> 23, 20u) - 7u;             // largest magnitude to [128, 256)
-          const float up = __builtin_bit_cast(float, (254u - top[u]) << 23) * sign;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[u][i] *= up;
-#pragma unroll
-          for (int p = 0; p < NP; ++p) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              int word = 0;
-              word = __builtin_amdgcn_cvt_pk_fp8_f32(x[u][4 * w], x[u][4 * w + 1], word, false);
-              word = __builtin_amdgcn_cvt_pk_fp8_f32(x[u][4 * w + 2], x[u][4 * w + 3], word, true);
-              q[rt][kk][p][u * 4 + w] = word;
-              x[u][4 * w] = (x[u][4 * w] - __builtin_amdgcn_cvt_f32_fp8(word, 0)) * 16.f;
-              x[u][4 * w + 1] = (x[u][4 * w + 1] - __builtin_amdgcn_cvt_f32_fp8(word, 1)) * 16.f;
-              x[u][4 * w + 2] = (x[u][4 * w + 2] - __builtin_amdgcn_cvt_f32_fp8(word, 2)) * 16.f;
-              x[u][4 * w + 3] = (x[u][4 * w + 3] - __builtin_amdgcn_cvt_f32_fp8(word, 3)) * 16.f;
-            }
-          }
-        }
-        // lane j gives the scale of group j: groups 0 and 1 are those of lanes 0 and 2 (first half), 2 and 3 of the second
-        const int from = n + 32 * (j & 1), t0 = __shfl((int)top[0], from), t1 = __shfl((int)top[1], from);
-        const int t = j < 2 ? t0 : t1;
-        q_byte[rt][kk] = t | (t - 4) << 8 | (t - 8) << 16;
-      }
+      load_queries<NG, BF>(src, there, sign, n, j, q[rt], q_byte[rt]);
     }
 
     auto step = [&](Tile<NG>& t, int at, bool careful) {
       const bool masked = at < span.all_lo || at + kTile > span.all_hi;
-      B8 p_hi[RT], p_lo[RT];
+      V4i p_hi[RT], p_lo[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float x[8];
@@ -287,25 +163,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
         }
         const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;       // nothing seen yet: weights of 2^-inf, not NaN
-        uint32_t bits[8];
+        float weight[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
-          sum[rt] += w;
-          bits[i] = __builtin_bit_cast(uint32_t, w);
+          weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
+          sum[rt] += weight[i];
         }
-        // the first part is cut off, not rounded: it takes no instruction but the one that joins two of them
-        V4i hi, lo;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          hi[i] = (int)__builtin_amdgcn_perm(bits[2 * i + 1], bits[2 * i], 0x07060302u);
-          const float r0 = __builtin_bit_cast(float, bits[2 * i]) - __builtin_bit_cast(float, bits[2 * i] & 0xFFFF0000u);
-          const float r1 = __builtin_bit_cast(float, bits[2 * i + 1]) - __builtin_bit_cast(float, bits[2 * i + 1] & 0xFFFF0000u);
-          const B2 r = {(__bf16)r0, (__bf16)r1};
-          lo[i] = __builtin_bit_cast(int, r);
-        }
-        p_hi[rt] = __builtin_bit_cast(B8, hi);
-        p_lo[rt] = __builtin_bit_cast(B8, lo);
+        parts_of<false>(weight, p_hi[rt], p_lo[rt]);
       }
       if (careful || at + kTile > seq.length) {
         // Tokens behind the sequence's end may hold anything: their factor becomes the least one.  In a careful pass that of values that are
@@ -338,18 +202,18 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
 #pragma unroll
           for (int k = 0; k < 4; k += 2) {
             const int b0 = k * NG + i, b1 = (k + 1) * NG + i;
-            const uint32_t v0 = __builtin_bit_cast(uint32_t, decode_at(t.value[u][b0 >> 2], t.value_byte[u][b0 >> 2], b0 & 3));
-            const uint32_t v1 = __builtin_bit_cast(uint32_t, decode_at(t.value[u][b1 >> 2], t.value_byte[u][b1 >> 2], b1 & 3));
+            const uint32_t v0 = decode_at<false>(t.value[u][b0 >> 2], t.value_byte[u][b0 >> 2], b0 & 3);
+            const uint32_t v1 = decode_at<false>(t.value[u][b1 >> 2], t.value_byte[u][b1 >> 2], b1 & 3);
             lower[u * 2 + k / 2] = (int)__builtin_amdgcn_perm(v1, v0, 0x05040100u);
             upper[u * 2 + k / 2] = (int)__builtin_amdgcn_perm(v1, v0, 0x07060302u);
           }
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          out[rt][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, lower), p_lo[rt], out[rt][2 * i], 0, 0, 0);
-          out[rt][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, upper), p_lo[rt], out[rt][2 * i + 1], 0, 0, 0);
-          out[rt][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, lower), p_hi[rt], out[rt][2 * i], 0, 0, 0);
-          out[rt][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, upper), p_hi[rt], out[rt][2 * i + 1], 0, 0, 0);
+          out[rt][2 * i] = multiply<false>(lower, p_lo[rt], out[rt][2 * i]);
+          out[rt][2 * i + 1] = multiply<false>(upper, p_lo[rt], out[rt][2 * i + 1]);
+          out[rt][2 * i] = multiply<false>(lower, p_hi[rt], out[rt][2 * i]);
+          out[rt][2 * i + 1] = multiply<false>(upper, p_hi[rt], out[rt][2 * i + 1]);
         }
       }
     };
@@ -460,9 +324,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
 }
 
 // The sums of a row's splits together.
-template <int NG, bool BF, int RT>
+template <int NG, bool BF>
 __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Grid g) {
-  constexpr int D = 32 * NG, R = 16 * RT, LANES = D / 4, GROUPS = 256 / LANES;      // a group of lanes takes a split at a time
+  constexpr int D = 32 * NG, LANES = D / 4, GROUPS = 256 / LANES;      // a group of lanes takes a split at a time
   __shared__ __align__(16) float lds[GROUPS][D];
   __shared__ float weight[kMostSplits], most_of[4], total_of[4];
   const int64_t id = blockIdx.x;
@@ -489,7 +353,7 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
   const int query = (int)(token - seq.first);
   if (query < 0 || query >= seq.queries) return;
   const int row = query * a.shared + h - head * a.shared;
-  const Span span = span_of(a, g, seq, row / R * R, R);
+  const Span span = span_of(a, g, seq, row / g.rows * g.rows);
   if (span.used <= 1) return;
   static_assert(kMostSplits == 256, "a thread has one split's maximum");
   const bool has = mine < span.used;
@@ -526,15 +390,20 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
 
 // Two tiles of rows share the decoded values where there are more rows than one has (beyond 128 channels the registers do not hold two).
 int row_tiles(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > 16 && a.pool.dim <= 128 ? 2 : 1; }
+// Rows from which the kernel for many rows takes a call.
+constexpr int kPromptRows = 64;
+bool is_prompt(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > kPromptRows; }
 
 Grid grid_of(const KvAttention& a) {
   Grid g{};
-  const int64_t rows = 16 * row_tiles(a), unit = kWaves * kTile;
-  g.row_blocks = (int32_t)(((int64_t)a.most_queries * a.shared + rows - 1) / rows);
-  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, wanted = (int64_t)device_cu_count() * 2;
-  const int64_t longest = std::max<int64_t>(1, std::min(a.longest, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest));
+  const bool prompt = is_prompt(a);
+  g.rows = prompt ? 16 * kWaves * prompt_row_tiles(a.pool.dim) : 16 * row_tiles(a);
+  g.unit = kWaves * kTile;
+  g.row_blocks = (int32_t)(((int64_t)a.most_queries * a.shared + g.rows - 1) / g.rows);
+  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, wanted = (int64_t)device_cu_count() * 2, unit = g.unit;
+  const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
   int64_t splits = others > 0 ? (wanted + others - 1) / others : 1;
-  splits = std::max<int64_t>(1, std::min({splits, (longest + 4 * unit - 1) / (4 * unit), (int64_t)256}));
+  splits = std::max<int64_t>(1, std::min({splits, (longest + 4 * unit - 1) / (4 * unit), (int64_t)kMostSplits}));
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
   g.splits = (int32_t)((longest + g.chunk - 1) / g.chunk);
   g.ordered = a.batch > 1 && a.batch <= 64 && others * g.splits > 3 * (int64_t)device_cu_count();
@@ -544,22 +413,37 @@ Grid grid_of(const KvAttention& a) {
 template <int NG, bool BF, int RT>
 int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
   constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + (2 + RT) * kWaves * 16);
-  const int64_t blocks = (int64_t)a.batch * a.pool.heads * g.row_blocks * g.splits, rows = a.tokens * a.heads;
+  const int64_t blocks = (int64_t)a.batch * a.pool.heads * g.row_blocks * g.splits;
   if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<NG, BF, RT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   hipLaunchKernelGGL((attention_kernel<NG, BF, RT>), dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, Launch{a, g});
   MACKO_HIP_TRY(hipGetLastError());
-  if (g.splits > 1) {
-    hipLaunchKernelGGL((join_kernel<NG, BF, RT>), dim3((unsigned)rows), dim3(256), 0, stream, a, g);
+  return MACKO_OK;
+}
+
+template <int NG, bool BF>
+int launch_type(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  int status = MACKO_OK;
+  bool one = true;
+  if (is_prompt(a)) {
+    status = launch_prompt(a, g, stream);
+    one = false;
+  } else if constexpr (NG <= 4) {
+    if (row_tiles(a) == 2) {
+      status = launch_of<NG, BF, 2>(a, g, stream);
+      one = false;
+    }
+  }
+  if (one) status = launch_of<NG, BF, 1>(a, g, stream);
+  if (status == MACKO_OK && g.splits > 1) {
+    hipLaunchKernelGGL((join_kernel<NG, BF>), dim3((unsigned)(a.tokens * a.heads)), dim3(256), 0, stream, a, g);
     MACKO_HIP_TRY(hipGetLastError());
   }
-  return MACKO_OK;
+  return status;
 }
 
 template <int NG>
 int launch_dim(const KvAttention& a, const Grid& g, hipStream_t stream) {
-  if constexpr (NG <= 4)
-    if (row_tiles(a) == 2) return a.type == MACKO_BF16 ? launch_of<NG, true, 2>(a, g, stream) : launch_of<NG, false, 2>(a, g, stream);
-  return a.type == MACKO_BF16 ? launch_of<NG, true, 1>(a, g, stream) : launch_of<NG, false, 1>(a, g, stream);
+  return a.type == MACKO_BF16 ? launch_type<NG, true>(a, g, stream) : launch_type<NG, false>(a, g, stream);
 }
 
 }  // namespace

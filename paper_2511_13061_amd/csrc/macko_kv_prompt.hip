@@ -1,0 +1,361 @@
+// Attention over the 4-bit cache for many rows of a sequence (a part of a prompt): there the vector units and the matrix cores are what bounds a
+// step, not memory.  The four wavefronts of a workgroup have rows of their own and go along the tokens together, 64 at a time:
+//   values   are decoded once for all of them, a quarter by each, into LDS, as the operand of the matrix instruction: a lane's 8 tokens of one
+//            channel lie together.  The steps are staggered: while step t is multiplied, t + 1 is decoded and t + 2 is on its way from memory.
+//            In fp16, which holds factors from 2^-19 to 2^12 exactly; a workgroup that meets another one starts again and takes bf16.
+//   weights  are one fp16 part (11 bits) for results in bf16, two for fp16; two parts of their type with values in bf16.
+//   scores   as in macko_kv_attention.hip: keys as they lie in memory.
+//   sums     of the weights come from the matrix cores too (a row of ones).
+#include "macko_kv_attention.h"
+
+namespace macko {
+namespace {
+
+constexpr int kStep = 64, kBlocks = kStep / 16, kWide = 1, kNan = 2;
+
+template <int NG, bool BF, int RT>
+__global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(const Launch args) {
+  const KvAttention& a = args.a;
+  const Grid& g = args.g;
+  constexpr int D = 32 * NG, NK = (NG + 3) / 4, NP = BF ? 2 : 3, R = 16 * RT * kWaves;
+  extern __shared__ __align__(16) V4i lds[];             // [2][2][2 NG][64]: 8 tokens of one channel, for a step, 32 of its tokens, 16 channels and a lane
+  uint32_t* const outside = reinterpret_cast<uint32_t*>(lds + 2 * 2 * 2 * NG * 64);     // [2][kWaves]: what look_over has found in a step's values
+  uint32_t* const lds_spoilt = outside + 2 * kWaves;     // [kWaves][RT][16]: groups in which a row sees what is not a number
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t pairs = (uint32_t)a.batch * a.pool.heads, bh = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int head = (int)(bh % a.pool.heads), split = (int)(rest / g.row_blocks);
+  int b = (int)(bh / a.pool.heads);
+  if (g.ordered) b = nth_longest(a, b, threadIdx.x & 63);
+  const Sequence seq = sequence_of(a, b);
+  const int32_t* const table = a.tables + b * a.table_stride;
+  const int64_t piece = kv_piece_bytes(int64_t{1} << a.pool.page_bits, D), page_stride = piece * a.pool.heads;
+  const uint8_t* const pool = a.pool.data + head * piece;
+  const int page_size = 1 << a.pool.page_bits;
+  const float unit = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f, sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
+  const float lift = kLift / unit;
+  const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
+
+  for (int first_row = (int)(rest % g.row_blocks) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
+    const Span span = span_of(a, g, seq, first_row);
+    if (split >= span.used) continue;
+    const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4;
+    const int begin = span.lo + split * span.chunk, end = span.hi - begin > span.chunk ? begin + span.chunk : span.hi;
+    const int last_block = (end - 1) >> 4;
+    bool bad = end > begin && (a.table_width == 0 || a.pool.pages == 0);
+    const bool any = end > begin && !bad;
+
+    V4i key[kBlocks][NK];
+    int key_byte[kBlocks][NK];
+    uint32_t value[NG], value_byte[NG];                  // of the wavefront's own block of a step
+    // A lane has the page of one block of 16 steps; they are looked up anew, half of them again, every 8.
+    int pages = 0;
+    auto entry = [&](int at) { return table[min(min((at >> 4) + lane, last_block) >> (a.pool.page_bits - 4), a.table_width - 1)]; };
+    auto take = [&](int at, int page) {
+      const bool fine = min((at >> 4) + lane, last_block) >> (a.pool.page_bits - 4) < a.table_width && page >= 0 && page < a.pool.pages;
+      bad = bad || __any(!fine);
+      pages = fine ? page : 0;
+    };
+    // Codes of a block, and how far behind them its factors lie
+    auto codes_of = [&](int at, int u, int slot, int64_t& bytes) {
+      const int in_page = (min((at >> 4) + u, last_block) << 4) & (page_size - 1);
+      bytes = page_size * D - in_page * (D / 2 - NG);
+      return pool + (int64_t)__builtin_amdgcn_readlane(pages, slot * kBlocks + u) * page_stride + in_page * (D / 2);
+    };
+    auto load_keys = [&](int at, int slot) {
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u) {
+        int64_t bytes;
+        const uint8_t* const codes = codes_of(at, u, slot, bytes);
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+          key[u][kk] = V4i{0, 0, 0, 0};
+          key_byte[u][kk] = 0;
+          if (kk * 4 + j < NG) {
+            key[u][kk] = *reinterpret_cast<const V4i*>(codes + (uint32_t)(n * (D / 2) + j * 16) + kk * 64);
+            key_byte[u][kk] = (codes + bytes)[(uint32_t)(n * NG + j) + kk * 4];
+          }
+        }
+      }
+    };
+    auto load_values = [&](int at, int slot) {
+      int64_t bytes;
+      const uint8_t* const codes = codes_of(at, wave, slot, bytes);
+      const uint32_t* const v = reinterpret_cast<const uint32_t*>(codes + page_size * (D / 2) + (uint32_t)((j * 16 + n) * (4 * NG)));
+      const uint32_t* const vb = reinterpret_cast<const uint32_t*>(codes + bytes + page_size * NG + (uint32_t)(j * (4 * NG)));
+#pragma unroll
+      for (int w = 0; w < NG; ++w) {
+        value[w] = v[w];
+        value_byte[w] = vb[w];
+      }
+    };
+    // What there is to see to in the wavefront's values of a step, of tokens that a row may see: kWide, factors beyond 2^-19 to 2^12 (bytes 108 to 139; 0 is
+    // a group of zeros), kNan, values that are not numbers.
+    auto look_over = [&](int at, int parity) {
+      uint32_t far = 0;                                   // each byte 0 to 31 once 108 is taken off (one below borrows, and shows that itself)
+#pragma unroll
+      for (int w = 0; w < NG; ++w) far |= value_byte[w] - 0x6C6C6C6Cu;
+      int what = 0;
+      if (__any((far & 0xE0E0E0E0u) != 0)) {
+        bool wide = false, nan = false;
+#pragma unroll
+        for (int k = 0; k < 4 * NG; ++k) {
+          const uint32_t byte = value_byte[k >> 2] >> 8 * (k & 3) & 255u;
+          const int token = at + wave * 16 + j * 4 + k / NG;
+          const bool counts = token >= span.first && token < end;
+          nan = nan || (counts && byte == 255u);
+          wide = wide || (counts && byte != 255u && byte > 139u) || (counts && byte < 108u && byte != 0u);
+        }
+        what = (__any(wide) ? kWide : 0) | (__any(nan) ? kNan : 0);
+      }
+      if (lane == 0) outside[parity * kWaves + wave] = what;
+    };
+    auto found = [&](int parity) {
+      const uint32_t* const o = outside + parity * kWaves;
+      return __builtin_amdgcn_readfirstlane((int)(o[0] | o[1] | o[2] | o[3]));
+    };
+    auto decode = [&](int at, int parity, int what, auto half) {
+      constexpr bool HALF = decltype(half)::value;
+      if (at < span.first || at + kStep > end || (what & kNan)) {      // what no row sees may be anything, values that are not numbers are left out
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int token = at + wave * 16 + j * 4 + k;
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            const int byte = k * NG + i, shift = 8 * (byte & 3);
+            if (token < span.first || token >= end || (value_byte[byte >> 2] >> shift & 255u) == 255u) value_byte[byte >> 2] &= ~(255u << shift);
+          }
+        }
+      }
+      uint2* const to = reinterpret_cast<uint2*>(lds + (parity * 2 + (wave >> 1)) * 2 * NG * 64 + lane) + (wave & 1);
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        uint32_t v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = decode_at<HALF>(value[(k * NG + i) >> 2], value_byte[(k * NG + i) >> 2], (k * NG + i) & 3);
+        to[(2 * i) * 128] = uint2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u)};
+        to[(2 * i + 1) * 128] = uint2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+      }
+    };
+
+    // the rows of this lane
+    int place[RT];
+    V8i q[RT][NK][NP];
+    int q_byte[RT][NK];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = first_row + (wave * RT + rt) * 16 + n, query = row / a.shared;
+      const bool there = row < seq.rows;
+      place[rt] = there ? seq.length - seq.queries + query : -1;
+      const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
+      load_queries<NG, BF>(src, there, sign, n, j, q[rt], q_byte[rt]);
+      __builtin_amdgcn_sched_barrier(0);                  // one tile of rows at a time, or the registers do not hold what lies between
+      if (lane < 16) lds_spoilt[(wave * RT + rt) * 16 + lane] = 0;
+    }
+
+    float top[RT];
+    V4f out[RT][2 * NG], total[RT];                      // the sum of the weights, the same in every row
+    // All steps; true: not to be done this way.
+    auto go = [&](auto half) {
+      constexpr bool HALF = decltype(half)::value;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        top[rt] = -INFINITY;
+        total[rt] = V4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 2 * NG; ++c) out[rt][c] = V4f{0.f, 0.f, 0.f, 0.f};
+      }
+      if (!any) return false;
+      // what is loaded ahead of the last step is its last block again
+      take(begin, entry(begin));
+      load_values(begin, 0);
+      load_keys(begin, 0);
+      look_over(begin, 0);
+      __syncthreads();
+      int now = found(0);
+      if (HALF && (now & kWide)) return true;
+      decode(begin, 0, now, half);
+      load_values(begin + kStep, 1);
+      look_over(begin + kStep, 1);
+      __syncthreads();
+      int ahead = 0;                                      // table entries on their way
+      for (int at = begin, parity = 0, slot = 0; at < end; at += kStep, parity ^= 1) {
+        const bool more = at + kStep < end;
+        const int next = more ? found(parity ^ 1) : 0;
+        if (HALF && (next & kWide)) return true;
+        if (more) decode(at + kStep, parity ^ 1, next, half);
+        if (now & kNan) {                                 // values that are not numbers have been left out: the rows that see them are marked
+#pragma unroll 1
+          for (int u = 0; u < kBlocks; ++u) {
+            const int in_page = (min((at >> 4) + u, last_block) << 4) & (page_size - 1);
+            const uint8_t* const piece_of = pool + (int64_t)__builtin_amdgcn_readlane(pages, slot * kBlocks + u) * page_stride;
+            const uint8_t* const vb = piece_of + page_size * (D + NG) + (in_page + j * 4) * NG;
+#pragma unroll 1
+            for (int k = 0; k < 4 * NG; ++k) {
+              const int token = at + u * 16 + j * 4 + k / NG;
+              if (vb[k] != 255 || token >= end) continue;
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt)
+                if ((uint32_t)(place[rt] - token) < reach) atomicOr(lds_spoilt + (wave * RT + rt) * 16 + n, 1u << k % NG);
+            }
+          }
+        }
+        // ---- weights
+        V4i p_hi[RT][2], p_lo[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float x[16];
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u) {
+            V4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) {
+              const V8i k8 = {key[u][kk][0], key[u][kk][1], key[u][kk][2], key[u][kk][3], 0, 0, 0, 0};
+              if (NP == 3) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NP - 1], s, 4, 0, 0, key_byte[u][kk], 2, q_byte[rt][kk]);
+              s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][1], s, 4, 0, 0, key_byte[u][kk], 1, q_byte[rt][kk]);
+              s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], s, 4, 0, 0, key_byte[u][kk], 0, q_byte[rt][kk]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * u + i] = s[i];
+          }
+          if (rt == RT - 1 && more) load_keys(at + kStep, slot + 1);      // in the registers of this step's
+          if (at < span.all_lo || at + kStep > span.all_hi) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int token = at + (i >> 2) * 16 + j * 4 + (i & 3);
+              if ((uint32_t)(place[rt] - token) >= reach) x[i] = -INFINITY;
+            }
+          }
+          float most = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) most = fmaxf(most, x[i]);
+          if (__any(most > top[rt] + lift)) {
+            float to = fmaxf(most, __shfl_xor(most, 16));
+            to = fmaxf(to, __shfl_xor(to, 32));
+            to = fmaxf(to, top[rt]);
+            const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
+            top[rt] = to;
+            total[rt] *= by;
+#pragma unroll
+            for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
+          }
+          const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
+#pragma unroll
+          for (int s = 0; s < 2; ++s) parts_of<HALF>(x + 8 * s, p_hi[rt][s], p_lo[rt][s]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (at + 2 * kStep < end) load_values(at + 2 * kStep, slot + 2);      // in the registers that the next step's have left
+        if (slot == 4) ahead = entry(at + 4 * kStep);
+        // ---- products
+        constexpr bool ONE = HALF && BF;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int one = HALF ? 0x3C003C00 : 0x3F803F80;
+          const V4i ones = {one, one, one, one};
+          const V4i* const from = lds + (parity * 2 + s) * 2 * NG * 64 + lane;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            if (!ONE) total[rt] = multiply<HALF>(ones, p_lo[rt][s], total[rt]);
+            total[rt] = multiply<HALF>(ones, p_hi[rt][s], total[rt]);
+          }
+#pragma unroll
+          for (int c = 0; c < 2 * NG; ++c) {
+            const V4i v = from[c * 64];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              if (!ONE) out[rt][c] = multiply<HALF>(v, p_lo[rt][s], out[rt][c]);
+              out[rt][c] = multiply<HALF>(v, p_hi[rt][s], out[rt][c]);
+            }
+          }
+        }
+        now = next;
+        look_over(at + 2 * kStep, parity);
+        if (++slot == 8) {
+          take(at + kStep, ahead);
+          slot = 0;
+        }
+        __syncthreads();
+      }
+      return false;
+    };
+    if (go(std::integral_constant<bool, true>{})) {
+      __syncthreads();
+      go(std::integral_constant<bool, false>{});
+    }
+
+    LaunchPtr e = (LaunchPtr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(e));
+    const int thread = later(threadIdx.x), row16 = thread & 15, quad = thread >> 4 & 3;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = first_row + (wave * RT + rt) * 16 + row16;
+      const uint32_t spoilt = lds_spoilt[(wave * RT + rt) * 16 + row16];
+      if (row >= seq.rows) continue;
+      const int query = row / e->a.shared, h = head * e->a.shared + row - query * e->a.shared;
+      const int64_t token = seq.first + query;
+      const float sum = bad ? NAN : total[rt][0], most = top[rt] * unit;
+      const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
+      const float r = span.used > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+      uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + quad * 4;
+      float* const partial = e->g.parts + part * D + quad * 4;
+#pragma unroll
+      for (int c = 0; c < 2 * NG; ++c) {
+        V4f o = out[rt][c] * r;
+        if (spoilt >> (c / 2) & 1) o = V4f{NAN, NAN, NAN, NAN};
+        if (span.used > 1) {
+          *reinterpret_cast<V4f*>(partial + c * 16) = o;
+        } else {
+          typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(2)));
+          *reinterpret_cast<Pair*>(dst + c * 16) = Pair{pack2<BF>(o[0], o[1]), pack2<BF>(o[2], o[3])};
+        }
+      }
+      if (quad > 0) continue;
+      if (span.used > 1) {
+        float* const ms = e->g.parts + e->a.tokens * e->a.heads * e->g.splits * D + part * 2;
+        ms[0] = most;
+        ms[1] = sum;
+      } else if (e->a.sums) {
+        e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+      }
+    }
+    __syncthreads();                                      // the marks are cleared for the next rows
+  }
+}
+
+template <int NG, bool BF>
+int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  constexpr int RT = NG <= 4 ? 2 : 1, lds = 16 * 2 * 2 * 2 * NG * 64 + 4 * (2 * kWaves + kWaves * RT * 16);
+  const void* const kernel = reinterpret_cast<const void*>(&prompt_kernel<NG, BF, RT>);
+  if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  const int64_t blocks = (int64_t)a.batch * a.pool.heads * g.row_blocks * g.splits;
+  hipLaunchKernelGGL((prompt_kernel<NG, BF, RT>), dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, Launch{a, g});
+  MACKO_HIP_TRY(hipGetLastError());
+  return MACKO_OK;
+}
+
+template <int NG>
+int launch_dim(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  return a.type == MACKO_BF16 ? launch_of<NG, true>(a, g, stream) : launch_of<NG, false>(a, g, stream);
+}
+
+}  // namespace
+
+int prompt_row_tiles(int dim) { return dim <= 128 ? 2 : 1; }
+
+int launch_prompt(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  switch (a.pool.dim / 32) {
+    case 1: return launch_dim<1>(a, g, stream);
+    case 2: return launch_dim<2>(a, g, stream);
+    case 3: return launch_dim<3>(a, g, stream);
+    case 4: return launch_dim<4>(a, g, stream);
+    case 5: return launch_dim<5>(a, g, stream);
+    case 6: return launch_dim<6>(a, g, stream);
+    case 7: return launch_dim<7>(a, g, stream);
+    case 8: return launch_dim<8>(a, g, stream);
+  }
+  return MACKO_E_UNSUPPORTED;
+}
+
+}  // namespace macko

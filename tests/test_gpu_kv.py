@@ -587,3 +587,85 @@ def test_native_calls_do_what_the_general_ones_do(monkeypatch):
         for a, c in zip(one if isinstance(one, tuple) else (one,), two if isinstance(two, tuple) else (two,)):
             assert type(a) is type(c), i
             assert (torch.equal(a, c) and a.dtype == c.dtype) if isinstance(a, torch.Tensor) else a == c, i
+
+
+# ---- many rows ----------------------------------------------------------------
+
+PROMPT = [
+    # dim, page, heads, kv heads, lengths, queries, window
+    (128, 16, 8, 2, [300], [100], 0), (128, 64, 4, 4, [130, 65, 64, 200], [130, 65, 64, 1], 0), (32, 16, 6, 2, [150, 30], [90, 30], 0), (64, 32, 40, 8, [700], [33], 0),
+    (96, 16, 3, 1, [90], [90], 0), (160, 16, 2, 1, [140, 77], [70, 40], 0), (192, 64, 3, 3, [300], [129], 0), (224, 16, 1, 1, [99], [80], 0), (256, 32, 8, 2, [260], [40], 0),
+    (128, 16, 4, 2, [400, 0, 90], [150, 3, 90], 0), (128, 16, 4, 2, [600], [200], 70), (64, 16, 2, 1, [500, 20], [300, 40], 1), (128, 128, 16, 1, [1000], [6], 333),
+    (128, 16, 2, 1, [2500], [90], 0), (256, 16, 2, 2, [1400, 3], [70, 70], 0), (64, 64, 66, 1, [3000, 700], [2, 2], 0),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(PROMPT)))
+def test_attention_of_many_rows(case, dtype):
+    dim, page, heads, kv_heads, lengths, queries, window = PROMPT[case]
+    g = rng(1000 + case)
+    cache = pool(g, sum(-(-n // page) for n in lengths) + 2, page, kv_heads, dim)
+    tables = sequences(g, cache, lengths)
+    fill(g, cache, tables, lengths)
+    start = np.concatenate([[0], np.cumsum(queries)])
+    q = normal(g, sum(queries), heads, dim, dtype=dtype, scale=1.5)
+    want = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, lengths, start, window=window)
+    for longest, most in ((max(lengths), max(queries)), (1, max(queries)), (None, 10 * max(queries))):
+        got, sums = cache.attend(q.cuda(), ints(tables), ints(lengths), start=ints(start), most_queries=most, window=window, longest=longest, sums=True)
+        check_attention(got, sums, *want, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("asked", [4, 90])
+@pytest.mark.parametrize("sizes", [(1e-4,), (2e-7, 1.0), (1.0, 3e4), (1e-6,), (0.0, 1.0), (0.0,), (1e-6, 1e4, 0.0)])
+def test_attention_values_of_any_size(sizes, asked, dtype):
+    """Values whose factors lie beyond what fp16 holds, in some tokens or all, groups of zeros among others."""
+    g = rng(41)
+    page, dim, length = 16, 128, 333
+    cache = pool(g, 22, page, 2, dim)
+    tables = sequences(g, cache, [length])
+    slots = tables[0, np.arange(length) // page] * page + np.arange(length) % page
+    k = normal(g, length, 2, dim, dtype=torch.bfloat16)
+    size = torch.tensor(sizes, dtype=torch.float64)[torch.arange(length) * 7 // 50 % len(sizes)]
+    v = (torch.randn((length, 2, dim), generator=g, dtype=torch.float64) * size[:, None, None]).bfloat16()
+    cache.append(None, k.cuda(), v.cuda(), None, ints(slots))
+    q = normal(g, asked, 4, dim, dtype=dtype)
+    want = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, [length], [0, asked])
+    got, sums = cache.attend(q.cuda(), ints(tables), ints([length]), start=ints([0, asked]), most_queries=asked, sums=True)
+    if dtype == torch.float16 and max(sizes) < 1e-3 and max(sizes) > 0:       # the results themselves are below fp16's normal numbers
+        share = want[2] * 2.0 ** -13 + 2.0 ** -15
+        close(got, want[0], dtype, (2 * share * want[3])[..., None])
+    else:
+        check_attention(got, sums, *want, dtype)
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_attention_of_many_rows_what_is_masked_has_no_effect(window):
+    """As above for the other kernel: NaN and an infinity in tokens that some rows see and others do not, wild bytes elsewhere, pages that are not needed."""
+    g = rng(51)
+    page, dim, heads, kv_heads, length, asked = 16, 64, 4, 2, 200, 120
+    clean, dirty = (pool(rng(i), 16, page, kv_heads, dim) for i in (1, 2))
+    tables = sequences(g, clean, [length])
+    for c in (clean, dirty):
+        fill(rng(9), c, tables, [length])
+    q = normal(g, asked, heads, dim)
+    call = dict(start=ints([0, asked]), most_queries=asked, window=window, sums=True)
+    want, total = clean.attend(q.cuda(), ints(tables), ints([length]), **call)
+    k, v = normal(g, 3, kv_heads, dim), normal(g, 3, kv_heads, dim)
+    v[0, 0, 40], v[1, 1, 3], k[2, 0, 9] = float("nan"), float("inf"), float("nan")
+    spots = (170, 131, 150)
+    dirty.append(None, k.cuda(), v.cuda(), None, ints([tables[0, t // page] * page + t % page for t in spots]))
+    if window:
+        tables[0, 0] = -7                                        # tokens 0 to 15: the first query is at place 80 and sees from 31 on
+    got, sums = dirty.attend(q.cuda(), ints(tables), ints([length]), **call)
+    place = np.arange(asked) + length - asked
+    free = [i for i in range(asked) if not any(t <= place[i] and (not window or t > place[i] - window) for t in spots)]
+    assert 40 < len(free) < asked and torch.equal(got[free], want[free]) and torch.equal(sums[free], total[free])
+    out, lse, reach, far = ref.attend(ref.to_numpy(q), dirty.data.cpu().numpy(), page, tables, [length], [0, asked], window=window)
+    assert np.array_equal(np.isnan(ref.to_numpy(got)), np.isnan(out)) and np.array_equal(np.isnan(ref.to_numpy(sums)), np.isnan(lse))
+    fine = ~np.isnan(out)
+    assert np.linalg.norm(ref.to_numpy(got)[fine] - out[fine]) <= 2.0 ** -11 * np.linalg.norm(out[fine])
+    tables[0, 9] = 99                                            # a page that rows from place 144 on need
+    again = ref.to_numpy(dirty.attend(q.cuda(), ints(tables), ints([length]), **call)[0])
+    assert np.isnan(again[place >= 144][:window or None]).all()
