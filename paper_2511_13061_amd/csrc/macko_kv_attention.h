@@ -24,8 +24,14 @@ struct Grid {
   int32_t rows, unit;              // rows of a block; tokens that a workgroup goes on by
   int32_t ordered;                 // long sequences first
   int64_t chunk;                   // tokens of a split, at least; a multiple of unit
-  float* parts;                    // [tokens * heads][splits][D], then [tokens * heads][splits][2]: maximum and sum
+  float* parts;                    // [tokens * heads][splits][D], then [tokens * heads][splits][2]: maximum and sum, then used_splits
 };
+
+// How many splits the tokens of a row are in, written with the first of them: [tokens * heads].
+template <class A, class G>
+__device__ inline int32_t* used_splits(const A& a, const G& g) {
+  return reinterpret_cast<int32_t*>(g.parts + a.tokens * a.heads * g.splits * (a.pool.dim + 2));
+}
 
 struct Launch {
   KvAttention a;

@@ -309,6 +309,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
             float* const ms = e->g.parts + e->a.tokens * e->a.heads * e->g.splits * D + part * 2;
             ms[0] = most;
             ms[1] = total;
+            if (split == 0) used_splits(e->a, e->g)[token * e->a.heads + h] = span.used;
           }
           continue;
         }
@@ -316,6 +317,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
         uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + channel;
 #pragma unroll
         for (int i = 0; i < 4; ++i) dst[i] = (uint16_t)to_bits<BF>(o[i] * r1);
+        if (e->g.splits > 1 && channel == 0) used_splits(e->a, e->g)[token * e->a.heads + h] = 1;
         if (e->a.sums && channel == 0) e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
       }
       __syncthreads();
@@ -323,41 +325,79 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   }
 }
 
-// The sums of a row's splits together.
+// The sums of a row's splits together; the rows whose tokens were not split have their results already.
+template <bool BF>
+__device__ inline void write_joined(const KvAttention& a, int64_t id, int channel, V4f o, float most, float total) {
+  const int h = (int)(id % a.heads);
+  const int64_t token = id / a.heads;
+  const float r = total == 0.f ? 0.f : 1.f / total;
+  typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(2)));
+  *reinterpret_cast<Pair*>(reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + h * a.out_head + channel) = Pair{pack2<BF>(o[0] * r, o[1] * r), pack2<BF>(o[2] * r, o[3] * r)};
+  if (a.sums && channel == 0) a.sums[id] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+}
+
+// Few splits: a wavefront has a row, a lane the maximum and the sum of one split.
+constexpr int kFewSplits = 16;
+template <int NG, bool BF>
+__global__ __launch_bounds__(256) void join_few_kernel(const KvAttention a, const Grid g) {
+  constexpr int D = 32 * NG, LANES = D / 4, GROUPS = LANES > 32 ? 1 : LANES > 16 ? 2 : LANES > 8 ? 4 : 8;      // a group of lanes takes a split at a time
+  const int64_t rows = a.tokens * a.heads, id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= rows) return;
+  const int lane = threadIdx.x & 63, group = lane / LANES, channel = lane % LANES * 4;
+  const float* const parts = g.parts + id * g.splits * D;
+  const float* const ms = g.parts + rows * g.splits * D + id * g.splits * 2;
+  // on their way before it is known how many splits there are
+  float top = -INFINITY, sum = 0.f;
+  if (lane < g.splits) top = ms[2 * lane], sum = ms[2 * lane + 1];
+  const int used = min(used_splits(a, g)[id], g.splits);
+  if (used <= 1) return;
+  if (lane >= used) top = -INFINITY, sum = 0.f;
+  float most = top;
+  for (int m = 1; m < kFewSplits; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+  most = __shfl(most, 0);
+  const float by = top == most ? 1.f : __builtin_amdgcn_exp2f(top - most);
+  float total = sum * by;
+  for (int m = 1; m < kFewSplits; m <<= 1) total += __shfl_xor(total, m);
+  total = __shfl(total, 0);
+  V4f o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < used; s0 += 4 * GROUPS) {
+    V4f part[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int s = s0 + k * GROUPS + group;
+      part[k] = V4f{0.f, 0.f, 0.f, 0.f};
+      if (group < GROUPS && s < used) part[k] = *reinterpret_cast<const V4f*>(parts + (int64_t)s * D + channel);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int s = s0 + k * GROUPS + group;
+      const float w = __shfl(by, s & 63);
+      if (s < used) o += part[k] * w;
+    }
+  }
+#pragma unroll
+  for (int m = GROUPS / 2; m > 0; m /= 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl(o[i], (lane + m * LANES) & 63);
+  }
+  if (group == 0) write_joined<BF>(a, id, channel, o, most, total);
+}
+
 template <int NG, bool BF>
 __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Grid g) {
-  constexpr int D = 32 * NG, LANES = D / 4, GROUPS = 256 / LANES;      // a group of lanes takes a split at a time
+  constexpr int D = 32 * NG, LANES = D / 4, GROUPS = 256 / LANES;
   __shared__ __align__(16) float lds[GROUPS][D];
   __shared__ float weight[kMostSplits], most_of[4], total_of[4];
-  const int64_t id = blockIdx.x;
+  const int64_t id = blockIdx.x, rows = a.tokens * a.heads;
   const float* const parts = g.parts + id * g.splits * D;
-  const float* const ms = g.parts + a.tokens * a.heads * g.splits * D + id * g.splits * 2;
+  const float* const ms = g.parts + rows * g.splits * D + id * g.splits * 2;
   const int mine = threadIdx.x, wave = mine >> 6, group = mine / LANES, channel = mine % LANES * 4;
-  // on their way before it is known how many splits there are
-  float my_top = 0.f, my_sum = 0.f;
-  if (mine < g.splits) my_top = ms[2 * mine], my_sum = ms[2 * mine + 1];
-  const int h = (int)(id % a.heads), head = h / a.shared;
-  const int64_t token = id / a.heads;
-  // the sequence of a token
-  int b = (int)token;
-  if (a.start) {
-    int lo = 0, hi = a.batch;                              // the last b with start[b] <= token
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.start[mid] <= token) lo = mid;
-      else hi = mid;
-    }
-    b = lo;
-  }
-  const Sequence seq = sequence_of(a, b);
-  const int query = (int)(token - seq.first);
-  if (query < 0 || query >= seq.queries) return;
-  const int row = query * a.shared + h - head * a.shared;
-  const Span span = span_of(a, g, seq, row / g.rows * g.rows);
-  if (span.used <= 1) return;
+  float top = -INFINITY, sum = 0.f;
   static_assert(kMostSplits == 256, "a thread has one split's maximum");
-  const bool has = mine < span.used;
-  const float top = has ? my_top : -INFINITY;
+  if (mine < g.splits) top = ms[2 * mine], sum = ms[2 * mine + 1];
+  const int used = min(used_splits(a, g)[id], g.splits);
+  if (used <= 1) return;
+  if (mine >= used) top = -INFINITY, sum = 0.f;
   float most = top;
   for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
   if ((mine & 63) == 0) most_of[wave] = most;
@@ -365,14 +405,14 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
   most = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
   const float by = top == most ? 1.f : __builtin_amdgcn_exp2f(top - most);
   weight[mine] = by;
-  float total = has ? my_sum * by : 0.f;
+  float total = sum * by;
   for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
   if ((mine & 63) == 0) total_of[wave] = total;
   __syncthreads();
   V4f o = {0.f, 0.f, 0.f, 0.f};
   if (group < GROUPS) {
 #pragma unroll 4
-    for (int s = group; s < span.used; s += GROUPS) o += *reinterpret_cast<const V4f*>(parts + (int64_t)s * D + channel) * weight[s];
+    for (int s = group; s < used; s += GROUPS) o += *reinterpret_cast<const V4f*>(parts + (int64_t)s * D + channel) * weight[s];
     *reinterpret_cast<V4f*>(&lds[group][channel]) = o;
   }
   __syncthreads();
@@ -380,12 +420,7 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
   o = V4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < GROUPS; ++k) o += *reinterpret_cast<const V4f*>(&lds[k][channel]);
-  total = (total_of[0] + total_of[1]) + (total_of[2] + total_of[3]);
-  const float r1 = total == 0.f ? 0.f : 1.f / total;
-  uint16_t* const dst = reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + h * a.out_head + channel;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) dst[i] = (uint16_t)to_bits<BF>(o[i] * r1);
-  if (a.sums && channel == 0) a.sums[id] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+  write_joined<BF>(a, id, channel, o, most, (total_of[0] + total_of[1]) + (total_of[2] + total_of[3]));
 }
 
 // Two tiles of rows share the decoded values where there are more rows than one has (beyond 128 channels the registers do not hold two).
@@ -435,7 +470,9 @@ int launch_type(const KvAttention& a, const Grid& g, hipStream_t stream) {
   }
   if (one) status = launch_of<NG, BF, 1>(a, g, stream);
   if (status == MACKO_OK && g.splits > 1) {
-    hipLaunchKernelGGL((join_kernel<NG, BF>), dim3((unsigned)(a.tokens * a.heads)), dim3(256), 0, stream, a, g);
+    const int64_t rows = a.tokens * a.heads;
+    if (g.splits <= kFewSplits) hipLaunchKernelGGL((join_few_kernel<NG, BF>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, g);
+    else hipLaunchKernelGGL((join_kernel<NG, BF>), dim3((unsigned)rows), dim3(256), 0, stream, a, g);
     MACKO_HIP_TRY(hipGetLastError());
   }
   return status;
@@ -460,7 +497,7 @@ bool kv_attention_fits(const KvAttention& a) {
 int64_t kv_attention_workspace(const KvAttention& a) {
   if (a.tokens == 0 || a.batch == 0) return 0;
   const Grid g = grid_of(a);
-  return g.splits > 1 ? a.tokens * a.heads * g.splits * (a.pool.dim + 2) : 0;
+  return g.splits > 1 ? a.tokens * a.heads * (g.splits * (int64_t)(a.pool.dim + 2) + 1) : 0;
 }
 
 int launch_kv_attention(const KvAttention& a, float* workspace, hipStream_t stream) {

@@ -200,76 +200,73 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
             }
           }
         }
-        // ---- weights
-        V4i p_hi[RT][2], p_lo[RT][2];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          float x[16];
+        for (int s = 0; s < 2; ++s) {                     // 32 tokens at a time: weights, then products
+          V4i p_hi[RT], p_lo[RT];
 #pragma unroll
-          for (int u = 0; u < kBlocks; ++u) {
-            V4f s = {0.f, 0.f, 0.f, 0.f};
+          for (int rt = 0; rt < RT; ++rt) {
+            float x[8];
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) {
-              const V8i k8 = {key[u][kk][0], key[u][kk][1], key[u][kk][2], key[u][kk][3], 0, 0, 0, 0};
-              if (NP == 3) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NP - 1], s, 4, 0, 0, key_byte[u][kk], 2, q_byte[rt][kk]);
-              s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][1], s, 4, 0, 0, key_byte[u][kk], 1, q_byte[rt][kk]);
-              s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], s, 4, 0, 0, key_byte[u][kk], 0, q_byte[rt][kk]);
+            for (int u = 0; u < 2; ++u) {
+              V4f y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int kk = 0; kk < NK; ++kk) {
+                const V4i k4 = key[2 * s + u][kk];
+                const V8i k8 = {k4[0], k4[1], k4[2], k4[3], 0, 0, 0, 0};
+                if (NP == 3) y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NP - 1], y, 4, 0, 0, key_byte[2 * s + u][kk], 2, q_byte[rt][kk]);
+                y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][1], y, 4, 0, 0, key_byte[2 * s + u][kk], 1, q_byte[rt][kk]);
+                y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], y, 4, 0, 0, key_byte[2 * s + u][kk], 0, q_byte[rt][kk]);
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[4 * u + i] = y[i];
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * u + i] = s[i];
-          }
-          if (rt == RT - 1 && more) load_keys(at + kStep, slot + 1);      // in the registers of this step's
-          if (at < span.all_lo || at + kStep > span.all_hi) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int token = at + (i >> 2) * 16 + j * 4 + (i & 3);
-              if ((uint32_t)(place[rt] - token) >= reach) x[i] = -INFINITY;
+            if (s == 1 && rt == RT - 1) {                 // in the registers of this step's, and in those that the next one's values have left
+              if (more) load_keys(at + kStep, slot + 1);
+              if (at + 2 * kStep < end) load_values(at + 2 * kStep, slot + 2);
             }
+            if (at < span.all_lo || at + kStep > span.all_hi) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int token = at + s * 32 + (i >> 2) * 16 + j * 4 + (i & 3);
+                if ((uint32_t)(place[rt] - token) >= reach) x[i] = -INFINITY;
+              }
+            }
+            const float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            if (__any(most > top[rt] + lift)) {
+              float to = fmaxf(most, __shfl_xor(most, 16));
+              to = fmaxf(to, __shfl_xor(to, 32));
+              to = fmaxf(to, top[rt]);
+              const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
+              top[rt] = to;
+              total[rt] *= by;
+#pragma unroll
+              for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
+            }
+            const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
+            parts_of<HALF>(x, p_hi[rt], p_lo[rt]);
           }
-          float most = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) most = fmaxf(most, x[i]);
-          if (__any(most > top[rt] + lift)) {
-            float to = fmaxf(most, __shfl_xor(most, 16));
-            to = fmaxf(to, __shfl_xor(to, 32));
-            to = fmaxf(to, top[rt]);
-            const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
-            top[rt] = to;
-            total[rt] *= by;
-#pragma unroll
-            for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
-          }
-          const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
-#pragma unroll
-          for (int s = 0; s < 2; ++s) parts_of<HALF>(x + 8 * s, p_hi[rt][s], p_lo[rt][s]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if (at + 2 * kStep < end) load_values(at + 2 * kStep, slot + 2);      // in the registers that the next step's have left
-        if (slot == 4) ahead = entry(at + 4 * kStep);
-        // ---- products
-        constexpr bool ONE = HALF && BF;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
+          constexpr bool ONE = HALF && BF;
           const int one = HALF ? 0x3C003C00 : 0x3F803F80;
           const V4i ones = {one, one, one, one};
           const V4i* const from = lds + (parity * 2 + s) * 2 * NG * 64 + lane;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
-            if (!ONE) total[rt] = multiply<HALF>(ones, p_lo[rt][s], total[rt]);
-            total[rt] = multiply<HALF>(ones, p_hi[rt][s], total[rt]);
+            if (!ONE) total[rt] = multiply<HALF>(ones, p_lo[rt], total[rt]);
+            total[rt] = multiply<HALF>(ones, p_hi[rt], total[rt]);
           }
 #pragma unroll
           for (int c = 0; c < 2 * NG; ++c) {
             const V4i v = from[c * 64];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-              if (!ONE) out[rt][c] = multiply<HALF>(v, p_lo[rt][s], out[rt][c]);
-              out[rt][c] = multiply<HALF>(v, p_hi[rt][s], out[rt][c]);
+              if (!ONE) out[rt][c] = multiply<HALF>(v, p_lo[rt], out[rt][c]);
+              out[rt][c] = multiply<HALF>(v, p_hi[rt], out[rt][c]);
             }
           }
         }
+        if (slot == 4) ahead = entry(at + 4 * kStep);
         now = next;
         look_over(at + 2 * kStep, parity);
         if (++slot == 8) {
@@ -316,9 +313,11 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
         float* const ms = e->g.parts + e->a.tokens * e->a.heads * e->g.splits * D + part * 2;
         ms[0] = most;
         ms[1] = sum;
-      } else if (e->a.sums) {
-        e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+        if (split == 0) used_splits(e->a, e->g)[token * e->a.heads + h] = span.used;
+        continue;
       }
+      if (e->g.splits > 1) used_splits(e->a, e->g)[token * e->a.heads + h] = 1;
+      if (e->a.sums) e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
     __syncthreads();                                      // the marks are cleared for the next rows
   }
