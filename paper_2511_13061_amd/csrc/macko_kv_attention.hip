@@ -11,6 +11,8 @@
 //            The lanes of S^T that hold a token's weights are those that P^T needs: nothing moves between lanes.
 // The four wavefronts of a workgroup take turns along the tokens and join their sums in LDS; long sequences are split over workgroups
 // too, whose unnormalised sums a second kernel joins.
+#include <cmath>
+
 #include "macko_kv_attention.h"
 
 namespace macko {
@@ -429,16 +431,43 @@ int row_tiles(const KvAttention& a) { return (int64_t)a.most_queries * a.shared 
 constexpr int kPromptRows = 64;
 bool is_prompt(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > kPromptRows; }
 
+// How many parts the tokens of a sequence are dealt out to: the number with the shortest estimate, in microseconds.  A workgroup goes on by 128 tokens (one
+// step of each wavefront, two for many rows) in the time that it takes alone, or that the workgroups of a compute unit take for one each where that is
+// longer: from memory (6 TB/s) or on the vector units.  Workgroups take turns where more of them come than fit, and each has 5 to begin and to end.  Joining costs
+// a launch, the sums' way through memory and something for each part.  Constants from 33 calls of 1 to 64 sequences of 256 to 131072 tokens, 1 to 512 queries, heads of 32 to 256
+// channels, with 1 to 128 parts each; the choice took 2 % longer than the best of these in the mean, 12 at worst.
+int64_t splits_of(const KvAttention& a, int64_t others, int64_t units, int64_t unit_bytes) {
+  static constexpr int kTry[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
+  static_assert(kMostSplits == 256, "the last one tried");
+  const double cus = device_cu_count(), rows = (double)a.tokens * a.heads;
+  const bool prompt = is_prompt(a), two = !prompt && row_tiles(a) == 2, wide = a.pool.dim > 128;
+  const double alone = prompt ? 5.0 : two ? 1.3 : wide ? 1.4 : 0.9, room = prompt ? (wide ? 1 : 2) : two ? 2 : wide ? 1 : 3;
+  const double share = std::max((double)unit_bytes * cus / 6.0e6, prompt ? 3.7 : two ? 0.8 : 0.45);
+  auto time = [&](int64_t splits) {
+    const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);
+    const double turns = groups <= 4.0 * room ? std::ceil(groups / room) : groups / room + 0.5;
+    const double join = splits > 1 ? 3.4 + 0.02 * (double)splits + rows * (double)splits * (a.pool.dim + 2) * 8.0 / 4.0e6 : 0.0;
+    return turns * (5.0 + steps * std::max(alone, busy * share)) + join;
+  };
+  int64_t best = 1;
+  double least = time(1);
+  for (const int splits : kTry) {
+    if (splits > units) break;
+    const double t = time(splits);
+    if (t < least) least = t, best = splits;
+  }
+  return best;
+}
+
 Grid grid_of(const KvAttention& a) {
   Grid g{};
   const bool prompt = is_prompt(a);
   g.rows = prompt ? 16 * kWaves * prompt_row_tiles(a.pool.dim) : 16 * row_tiles(a);
   g.unit = kWaves * kTile;
   g.row_blocks = (int32_t)(((int64_t)a.most_queries * a.shared + g.rows - 1) / g.rows);
-  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, wanted = (int64_t)device_cu_count() * 2, unit = g.unit;
+  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, unit = g.unit;
   const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
-  int64_t splits = others > 0 ? (wanted + others - 1) / others : 1;
-  splits = std::max<int64_t>(1, std::min({splits, (longest + 4 * unit - 1) / (4 * unit), (int64_t)kMostSplits}));
+  const int64_t splits = splits_of(a, others, (longest + unit - 1) / unit, kv_piece_bytes(unit, a.pool.dim));
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
   g.splits = (int32_t)((longest + g.chunk - 1) / g.chunk);
   g.ordered = a.batch > 1 && a.batch <= 64 && others * g.splits > 3 * (int64_t)device_cu_count();
