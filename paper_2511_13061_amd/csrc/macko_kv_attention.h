@@ -23,6 +23,7 @@ struct Grid {
   int32_t row_blocks, splits;      // of a sequence's rows and of its tokens, at most
   int32_t rows, unit;              // rows of a block; tokens that a workgroup goes on by
   int32_t ordered;                 // long sequences first
+  uint32_t shared_inverse;         // 2^32 / a.shared, rounded up; 0 for 1
   int64_t chunk;                   // tokens of a split, at least; a multiple of unit
   float* parts;                    // [tokens * heads][splits][D], then [tokens * heads][splits][2]: maximum and sum, then used_splits
 };
@@ -39,35 +40,53 @@ struct Launch {
 };
 typedef const __attribute__((address_space(4))) Launch* LaunchPtr;
 
+// Read through the scalar cache: nothing writes them while a kernel runs.
+__device__ inline int32_t constant(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)p; }
+
 struct Sequence {
   int length, first, queries, rows;
 };
 __device__ inline Sequence sequence_of(const KvAttention& a, int b) {
   Sequence s;
-  s.length = min(max(0, a.lengths[b]), kMostTokens);
-  s.first = a.start ? min(max(a.start[b], 0), (int)a.tokens) : b;
-  s.queries = a.start ? min(max(a.start[b + 1], s.first), (int)a.tokens) - s.first : 1;
+  s.length = min(max(0, constant(a.lengths + b)), kMostTokens);
+  s.first = a.start ? min(max(constant(a.start + b), 0), (int)a.tokens) : b;
+  s.queries = a.start ? min(max(constant(a.start + b + 1), s.first), (int)a.tokens) - s.first : 1;
   s.rows = s.queries * a.shared;
   return s;
 }
 
-// The tokens that the rows first_row .. of a block see, and how they are split.
+// Rows of a block: row r belongs to query r / shared.  Behind the first one's the quotient is small, and exact as a product (shared is at most 2^15).
+struct Rows {
+  int first, query;                // the block's first row, and its query
+  __device__ int query_of(const KvAttention& a, const Grid& g, int row) const {
+    const uint32_t more = (uint32_t)(row - query * a.shared);
+    return query + (int)(g.shared_inverse ? __umulhi(more, g.shared_inverse) : more);
+  }
+};
+__device__ inline Rows rows_of(const KvAttention& a, int first_row) { return Rows{first_row, first_row == 0 ? 0 : first_row / a.shared}; }
+
+// The tokens that the rows of a block see, and how they are split.
 struct Span {
   int first, lo, hi, chunk, used;  // [first, hi); lo: first, down to a multiple of 16
   int all_lo, all_hi;              // every row of the block sees [all_lo, all_hi)
 };
-__device__ inline Span span_of(const KvAttention& a, const Grid& g, const Sequence& s, int first_row) {
+__device__ inline Span span_of(const KvAttention& a, const Grid& g, const Sequence& s, const Rows& rows) {
   Span p;
-  const int qa = first_row / a.shared, qb = min(first_row + g.rows - 1, s.rows - 1) / a.shared, offset = s.length - s.queries;
+  const int qa = rows.query, qb = rows.query_of(a, g, min(rows.first + g.rows - 1, s.rows - 1)), offset = s.length - s.queries;
   p.hi = min(max(offset + qb + 1, 0), s.length);
   p.all_hi = min(max(offset + qa + 1, 0), s.length);
   const int lo = a.window ? max(offset + qa - a.window + 1, 0) : 0;
   p.all_lo = a.window ? max(offset + qb - a.window + 1, 0) : 0;
   p.first = min(lo, p.hi);
   p.lo = p.first & ~15;
-  const int range = max(p.hi - p.lo, 0);
-  p.chunk = max((int)g.chunk, (int)(((unsigned)range + g.splits * g.unit - 1) / (unsigned)(g.splits * g.unit)) * g.unit);
-  p.used = max(1, (range + p.chunk - 1) / p.chunk);
+  p.chunk = kMostTokens;
+  p.used = 1;
+  if (g.splits > 1) {
+    const int range = max(p.hi - p.lo, 0);
+    p.chunk = (int)g.chunk;
+    if ((int64_t)p.chunk * g.splits < range) p.chunk = (int)(((unsigned)range + g.splits * g.unit - 1) / (unsigned)(g.splits * g.unit)) * g.unit;      // longer than was said
+    p.used = max(1, (int)(((unsigned)range + p.chunk - 1) / (unsigned)p.chunk));
+  }
   return p;
 }
 
@@ -83,6 +102,18 @@ __device__ inline int nth_longest(const KvAttention& a, int n, int lane) {
 #pragma unroll
   for (int m = 0; m < 64; ++m) longer += __builtin_amdgcn_readlane(key, m) > key;
   return __builtin_ctzll(__ballot(longer == n && lane < a.batch));
+}
+
+// Four values as 8-bit numbers, and 16 times what they leave over in their place.
+__device__ inline int part_of(float* x) {
+  int word = 0;
+  word = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], word, false);
+  word = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], word, true);
+  x[0] = (x[0] - __builtin_amdgcn_cvt_f32_fp8(word, 0)) * 16.f;
+  x[1] = (x[1] - __builtin_amdgcn_cvt_f32_fp8(word, 1)) * 16.f;
+  x[2] = (x[2] - __builtin_amdgcn_cvt_f32_fp8(word, 2)) * 16.f;
+  x[3] = (x[3] - __builtin_amdgcn_cvt_f32_fp8(word, 3)) * 16.f;
+  return word;
 }
 
 // Lane (n, j) = lane % 16, lane / 16 of the queries' operand for one tile of rows: row n, 8-bit parts, each 16 times what the one before left over, and a
@@ -115,16 +146,7 @@ __device__ inline void load_queries(const uint16_t* src, bool there, float sign,
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          int word = 0;
-          word = __builtin_amdgcn_cvt_pk_fp8_f32(x[u][4 * w], x[u][4 * w + 1], word, false);
-          word = __builtin_amdgcn_cvt_pk_fp8_f32(x[u][4 * w + 2], x[u][4 * w + 3], word, true);
-          q[kk][p][u * 4 + w] = word;
-          x[u][4 * w] = (x[u][4 * w] - __builtin_amdgcn_cvt_f32_fp8(word, 0)) * 16.f;
-          x[u][4 * w + 1] = (x[u][4 * w + 1] - __builtin_amdgcn_cvt_f32_fp8(word, 1)) * 16.f;
-          x[u][4 * w + 2] = (x[u][4 * w + 2] - __builtin_amdgcn_cvt_f32_fp8(word, 2)) * 16.f;
-          x[u][4 * w + 3] = (x[u][4 * w + 3] - __builtin_amdgcn_cvt_f32_fp8(word, 3)) * 16.f;
-        }
+        for (int w = 0; w < 4; ++w) q[kk][p][u * 4 + w] = part_of(x[u] + 4 * w);
       }
     }
     // lane j gives the scale of group j: groups 0 and 1 are those of lanes 0 and 2 (first half), 2 and 3 of the second

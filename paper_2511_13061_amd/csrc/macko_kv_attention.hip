@@ -39,11 +39,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   float* const lds_max = lds + kWaves * 16 * LD;
   float* const lds_sum = lds_max + kWaves * 16;
   uint32_t* const lds_spoilt = reinterpret_cast<uint32_t*>(lds_sum + kWaves * 16);      // [RT][kWaves][16]: groups in which a row sees what is not a number
+  uint32_t* const lds_q = lds_spoilt + RT * kWaves * 16;                                // [RT][NK][NP][64][8]
+  uint8_t* const lds_byte = reinterpret_cast<uint8_t*>(lds_q + RT * NK * NP * 512);     // [R][NG]
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t pairs = (uint32_t)a.batch * a.pool.heads, bh = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int head = (int)(bh % a.pool.heads), split = (int)(rest / g.row_blocks);
-  int b = (int)(bh / a.pool.heads);
+  const int head = blockIdx.x, split = g.splits == 1 ? 0 : g.row_blocks == 1 ? (int)blockIdx.z : (int)blockIdx.z / g.row_blocks, row_block = (int)blockIdx.z - split * g.row_blocks;
+  int b = blockIdx.y;
   if (g.ordered) b = nth_longest(a, b, threadIdx.x & 63);
   const Sequence seq = sequence_of(a, b);
   const int32_t* const table = a.tables + b * a.table_stride;
@@ -55,8 +56,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   const float lift = kLift / unit;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
-  for (int first_row = (int)(rest % g.row_blocks) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
-    const Span span = span_of(a, g, seq, first_row);
+  for (int first_row = row_block * R; first_row < seq.rows; first_row += g.row_blocks * R) {
+    const Rows rows = rows_of(a, first_row);
+    const Span span = span_of(a, g, seq, rows);
     if (split >= span.used) continue;
     // What follows from the lane is worked out here and again behind the steps (later(...)): kept from outside the loop it would hold registers.
     const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4;
@@ -110,7 +112,6 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       load(one, mine, 0);
     }
 
-    // rows of this lane
     if (lane < 16) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) lds_spoilt[(rt * kWaves + wave) * 16 + lane] = 0;
@@ -118,13 +119,59 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
     int place[RT];                                        // of a row's query: it sees the tokens t with 0 <= place - t < reach
     V8i q[RT][NK][NP];
     int q_byte[RT][NK];
+    // The queries' operand (load_queries says what it is), 8 channels of a row by each thread, through LDS to the lanes of all wavefronts.
+    constexpr int kChunks = R * 4 * NG, kTurns = (kChunks + 64 * kWaves - 1) / (64 * kWaves);
+#pragma unroll
+    for (int turn = 0; turn < kTurns; ++turn) {
+      const int chunk = turn * 64 * kWaves + (wave * 64 + lane), r = chunk / (4 * NG), c = chunk % (4 * NG);
+      if (chunk >= kChunks) break;
+      const int row = first_row + r, query = rows.query_of(a, g, row);
+      Packed8 raw = {0, 0, 0, 0};
+      if (row < seq.rows)
+        raw = *reinterpret_cast<const Packed8Any*>(reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token +
+                                                   (int64_t)(head * a.shared + row - query * a.shared) * a.q_head + c * 8);
+      float x[8];
+      unpack8<BF>(raw, x);
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = max(most, __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu);
+      most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xF, 0xF, true));      // the quad has a group
+      most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4E, 0xF, 0xF, true));
+      const uint32_t byte = max(most >> 23, 20u) - 7u;
+      const float up = __builtin_bit_cast(float, (254u - byte) << 23) * sign;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= up;
+      uint32_t* to = lds_q + (((r >> 4) * NK + (c >> 4)) * NP * 64 + ((c & 7) >> 1) * 16 + (r & 15)) * 8 + ((c & 8) >> 1) + (c & 1) * 2;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        uint2 words;
+        words.x = (uint32_t)part_of(x);
+        words.y = (uint32_t)part_of(x + 4);
+        *reinterpret_cast<uint2*>(to + p * 512) = words;
+      }
+      if ((c & 3) == 0) lds_byte[r * NG + (c >> 2)] = (uint8_t)byte;
+    }
+    __syncthreads();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int row = first_row + rt * 16 + n, query = row / a.shared;
-      const bool there = row < seq.rows;
-      place[rt] = there ? seq.length - seq.queries + query : -1;
-      const uint16_t* src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
-      load_queries<NG, BF>(src, there, sign, n, j, q[rt], q_byte[rt]);
+      const int row = first_row + rt * 16 + n;
+      place[rt] = row < seq.rows ? seq.length - seq.queries + rows.query_of(a, g, row) : -1;
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const V4i* const from = reinterpret_cast<const V4i*>(lds_q + (((rt * NK + kk) * NP + p) * 64 + lane) * 8);
+          V4i half[2] = {from[0], from[1]};
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if (NG % 4 != 0 && kk * 128 + u * 64 + j * 16 >= D) half[u] = V4i{0, 0, 0, 0};      // no such channels
+#pragma unroll
+            for (int w = 0; w < 4; ++w) q[rt][kk][p][u * 4 + w] = half[u][w];
+          }
+        }
+        const int t = kk * 4 + j < NG ? lds_byte[(rt * 16 + n) * NG + kk * 4 + j] : 20;
+        q_byte[rt][kk] = t | (t - 4) << 8 | (t - 8) << 16;
+      }
     }
 
     auto step = [&](Tile<NG>& t, int at, bool careful) {
@@ -220,6 +267,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       }
     };
 
+    bool again, marked = false;
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
@@ -255,14 +303,17 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       }
       // A value that is not a number reaches every row of its tile, with weight 0 where it is not seen: then the tokens are gone through
       // again, carefully.  Nothing but such values gets here.
-      bool nan = false;
+      float all[4] = {0.f, 0.f, 0.f, 0.f};                // infinities of both signs make one too: that costs time alone
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) nan = nan || out[rt][c][i] != out[rt][c][i];
-      if (!__any(nan)) break;
+          for (int i = 0; i < 4; ++i) all[i] += out[rt][c][i];
+      const float one_of = (all[0] + all[1]) + (all[2] + all[3]);
+      again = pass == 0 && __any(one_of != one_of);
+      if (!again) break;
+      marked = true;
     }
 
     // What the results need of the arguments is read again here, rather than kept in registers through the steps.
@@ -275,14 +326,15 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       sum[rt] += __shfl_xor(sum[rt], 16);
       sum[rt] += __shfl_xor(sum[rt], 32);
       if (bad) sum[rt] = NAN;
-      const uint32_t spoilt = lds_spoilt[(rt * kWaves + wave) * 16 + row16];
+      if (marked) {
+        const uint32_t spoilt = lds_spoilt[(rt * kWaves + wave) * 16 + row16];
+#pragma unroll
+        for (int c = 0; c < 2 * NG; ++c)
+          if (spoilt >> (c / 2) & 1) out[rt][c] = V4f{NAN, NAN, NAN, NAN};
+      }
       float* const mine = lds + (wave * 16 + row16) * LD;
 #pragma unroll
-      for (int c = 0; c < 2 * NG; ++c) {
-        V4f o = out[rt][c];
-        if (spoilt >> (c / 2) & 1) o = V4f{NAN, NAN, NAN, NAN};
-        *reinterpret_cast<V4f*>(mine + c * 16 + quad * 4) = o;
-      }
+      for (int c = 0; c < 2 * NG; ++c) *reinterpret_cast<V4f*>(mine + c * 16 + quad * 4) = out[rt][c];
       if (quad == 0) {
         lds_max[wave * 16 + row16] = top[rt] * unit;
         lds_sum[wave * 16 + row16] = sum[rt];
@@ -302,7 +354,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           total += lds_sum[w * 16 + r] * by;
           o += *reinterpret_cast<const V4f*>(lds + (w * 16 + r) * LD + channel) * by;
         }
-        const int query = row / e->a.shared, h = head * e->a.shared + row - query * e->a.shared;
+        const int query = rows.query_of(a, g, row), h = head * e->a.shared + row - query * e->a.shared;
         const int64_t token = first_of_sequence + query;
         if (span.used > 1) {
           const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
@@ -316,9 +368,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           continue;
         }
         const float r1 = total == 0.f ? 0.f : 1.f / total;
-        uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + channel;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dst[i] = (uint16_t)to_bits<BF>(o[i] * r1);
+        typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(2)));
+        *reinterpret_cast<Pair*>(reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + channel) =
+            Pair{pack2<BF>(o[0] * r1, o[1] * r1), pack2<BF>(o[2] * r1, o[3] * r1)};
         if (e->g.splits > 1 && channel == 0) used_splits(e->a, e->g)[token * e->a.heads + h] = 1;
         if (e->a.sums && channel == 0) e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
       }
@@ -431,6 +483,8 @@ int row_tiles(const KvAttention& a) { return (int64_t)a.most_queries * a.shared 
 constexpr int kPromptRows = 64;
 bool is_prompt(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > kPromptRows; }
 
+constexpr int64_t kMostGrid = 65535;       // of a launch's second and third dimension
+
 // How many parts the tokens of a sequence are dealt out to: the number with the shortest estimate, in microseconds.  A workgroup goes on by 128 tokens (one
 // step of each wavefront, two for many rows) in the time that it takes alone, or that the workgroups of a compute unit take for one each where that is
 // longer: from memory (6 TB/s) or on the vector units.  Workgroups take turns where more of them come than fit, and each has 5 to begin and to end.  Joining costs
@@ -464,22 +518,23 @@ Grid grid_of(const KvAttention& a) {
   const bool prompt = is_prompt(a);
   g.rows = prompt ? 16 * kWaves * prompt_row_tiles(a.pool.dim) : 16 * row_tiles(a);
   g.unit = kWaves * kTile;
-  g.row_blocks = (int32_t)(((int64_t)a.most_queries * a.shared + g.rows - 1) / g.rows);
-  const int64_t others = (int64_t)a.batch * a.pool.heads * g.row_blocks, unit = g.unit;
+  const int64_t row_blocks = ((int64_t)a.most_queries * a.shared + g.rows - 1) / g.rows;
+  g.shared_inverse = a.shared == 1 ? 0u : (uint32_t)(((uint64_t{1} << 32) + a.shared - 1) / a.shared);
+  const int64_t others = (int64_t)a.batch * a.pool.heads * row_blocks, unit = g.unit;
   const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
   const int64_t splits = splits_of(a, others, (longest + unit - 1) / unit, kv_piece_bytes(unit, a.pool.dim));
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
   g.splits = (int32_t)((longest + g.chunk - 1) / g.chunk);
+  g.row_blocks = (int32_t)std::min(row_blocks, kMostGrid / g.splits);      // of a launch: a workgroup goes on to others
   g.ordered = a.batch > 1 && a.batch <= 64 && others * g.splits > 3 * (int64_t)device_cu_count();
   return g;
 }
 
 template <int NG, bool BF, int RT>
 int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
-  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + (2 + RT) * kWaves * 16);
-  const int64_t blocks = (int64_t)a.batch * a.pool.heads * g.row_blocks * g.splits;
+  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + (2 + RT) * kWaves * 16 + RT * ((NG + 3) / 4) * (BF ? 2 : 3) * 512) + 16 * RT * NG;
   if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<NG, BF, RT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-  hipLaunchKernelGGL((attention_kernel<NG, BF, RT>), dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, Launch{a, g});
+  hipLaunchKernelGGL((attention_kernel<NG, BF, RT>), dim3((unsigned)a.pool.heads, (unsigned)a.batch, (unsigned)(g.row_blocks * g.splits)), dim3(64 * kWaves), lds, stream, Launch{a, g});
   MACKO_HIP_TRY(hipGetLastError());
   return MACKO_OK;
 }
@@ -516,11 +571,9 @@ int launch_dim(const KvAttention& a, const Grid& g, hipStream_t stream) {
 
 bool kv_attention_fits(const KvAttention& a) {
   if (a.tokens == 0 || a.batch == 0) return true;
-  constexpr int64_t kMost = (int64_t{1} << 24) - 1;       // workgroups of a launch of 256 threads each
-  const int64_t rows = a.tokens * a.heads, pairs = (int64_t)a.batch * a.pool.heads;
-  if (rows > kMostTokens || pairs > kMost) return false;
-  const Grid g = grid_of(a);
-  return pairs * g.row_blocks <= kMost && pairs * g.row_blocks * g.splits <= kMost && (g.splits == 1 || rows <= kMost);
+  constexpr int64_t kMost = (int64_t{1} << 24) - 1;       // workgroups in a row of a launch's, of 256 threads each
+  const int64_t rows = a.tokens * a.heads;
+  return rows <= kMostTokens && a.batch <= kMostGrid && a.shared <= 32768 && (rows <= kMost || grid_of(a).splits == 1);
 }
 
 int64_t kv_attention_workspace(const KvAttention& a) {

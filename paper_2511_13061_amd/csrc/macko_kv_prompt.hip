@@ -23,9 +23,8 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
   uint32_t* const lds_spoilt = outside + 2 * kWaves;     // [kWaves][RT][16]: groups in which a row sees what is not a number
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t pairs = (uint32_t)a.batch * a.pool.heads, bh = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int head = (int)(bh % a.pool.heads), split = (int)(rest / g.row_blocks);
-  int b = (int)(bh / a.pool.heads);
+  const int head = blockIdx.x, split = g.splits == 1 ? 0 : g.row_blocks == 1 ? (int)blockIdx.z : (int)blockIdx.z / g.row_blocks, row_block = (int)blockIdx.z - split * g.row_blocks;
+  int b = blockIdx.y;
   if (g.ordered) b = nth_longest(a, b, threadIdx.x & 63);
   const Sequence seq = sequence_of(a, b);
   const int32_t* const table = a.tables + b * a.table_stride;
@@ -36,8 +35,9 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
   const float lift = kLift / unit;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
-  for (int first_row = (int)(rest % g.row_blocks) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
-    const Span span = span_of(a, g, seq, first_row);
+  for (int first_row = row_block * R; first_row < seq.rows; first_row += g.row_blocks * R) {
+    const Rows rows = rows_of(a, first_row);
+    const Span span = span_of(a, g, seq, rows);
     if (split >= span.used) continue;
     const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4;
     const int begin = span.lo + split * span.chunk, end = span.hi - begin > span.chunk ? begin + span.chunk : span.hi;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
     int q_byte[RT][NK];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int row = first_row + (wave * RT + rt) * 16 + n, query = row / a.shared;
+      const int row = first_row + (wave * RT + rt) * 16 + n, query = rows.query_of(a, g, row);
       const bool there = row < seq.rows;
       place[rt] = there ? seq.length - seq.queries + query : -1;
       const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
       const int row = first_row + (wave * RT + rt) * 16 + row16;
       const uint32_t spoilt = lds_spoilt[(wave * RT + rt) * 16 + row16];
       if (row >= seq.rows) continue;
-      const int query = row / e->a.shared, h = head * e->a.shared + row - query * e->a.shared;
+      const int query = rows.query_of(a, g, row), h = head * e->a.shared + row - query * e->a.shared;
       const int64_t token = seq.first + query;
       const float sum = bad ? NAN : total[rt][0], most = top[rt] * unit;
       const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
@@ -328,8 +328,7 @@ int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
   constexpr int RT = NG <= 4 ? 2 : 1, lds = 16 * 2 * 2 * 2 * NG * 64 + 4 * (2 * kWaves + kWaves * RT * 16);
   const void* const kernel = reinterpret_cast<const void*>(&prompt_kernel<NG, BF, RT>);
   if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-  const int64_t blocks = (int64_t)a.batch * a.pool.heads * g.row_blocks * g.splits;
-  hipLaunchKernelGGL((prompt_kernel<NG, BF, RT>), dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, Launch{a, g});
+  hipLaunchKernelGGL((prompt_kernel<NG, BF, RT>), dim3((unsigned)a.pool.heads, (unsigned)a.batch, (unsigned)(g.row_blocks * g.splits)), dim3(64 * kWaves), lds, stream, Launch{a, g});
   MACKO_HIP_TRY(hipGetLastError());
   return MACKO_OK;
 }
