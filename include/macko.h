@@ -475,10 +475,14 @@ MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const
  * key/value head h / (heads / kv_heads).
  *   out = sum over seen t of softmax(scale * q.k_t) v_t,   sums = log sum exp(scale * q.k_t)
  * A query that sees nothing gets zeros and a sum of -infinity.  What lies in
- * tokens that no query sees, in the rest of pages and in table entries beyond the
- * length has no effect, NaN included.  A table entry that is needed and names no
- * page, or is missing (length > table_width * page_size), makes the results of the
- * queries that need it NaN.
+ * tokens that a query does not see, in the rest of pages and in table entries that no
+ * query of the sequence needs has no effect on it, NaN included (values that other
+ * queries see may decide how a query's own are multiplied, and change its last place).  A table entry that a
+ * query needs and that names no page, or is missing (length > table_width * page_size), makes its
+ * results NaN, and may make those of the sequence's other queries NaN.  Rows of q that
+ * are no sequence's are left with any content.
+ * Limits (MACKO_E_UNSUPPORTED): batch <= 65535, tokens * heads <= 2^30, 32768 heads to a
+ * key/value head; lengths above 2^30 count as 2^30.
  * most_queries and longest are upper bounds that size the launch (queries of one
  * sequence, tokens of one sequence): too small costs time, not correctness.
  * One launch, two where long sequences are split; workspace_dev:

@@ -504,6 +504,7 @@ int64_t splits_of(const KvAttention& a, int64_t others, int64_t units, int64_t u
     return turns * (5.0 + steps * std::max(alone, busy * share)) + join;
   };
   int64_t best = 1;
+  if (a.tokens * a.heads >= int64_t{1} << 24) return best;      // a join has a workgroup a row, and a launch fewer than 2^32 threads
   double least = time(1);
   for (const int splits : kTry) {
     if (splits > units) break;
@@ -571,9 +572,8 @@ int launch_dim(const KvAttention& a, const Grid& g, hipStream_t stream) {
 
 bool kv_attention_fits(const KvAttention& a) {
   if (a.tokens == 0 || a.batch == 0) return true;
-  constexpr int64_t kMost = (int64_t{1} << 24) - 1;       // workgroups in a row of a launch's, of 256 threads each
   const int64_t rows = a.tokens * a.heads;
-  return rows <= kMostTokens && a.batch <= kMostGrid && a.shared <= 32768 && (rows <= kMost || grid_of(a).splits == 1);
+  return rows <= kMostTokens && a.batch <= kMostGrid && a.shared <= 32768;
 }
 
 int64_t kv_attention_workspace(const KvAttention& a) {

@@ -669,3 +669,15 @@ def test_attention_of_many_rows_what_is_masked_has_no_effect(window):
     tables[0, 9] = 99                                            # a page that rows from place 144 on need
     again = ref.to_numpy(dirty.attend(q.cuda(), ints(tables), ints([length]), **call)[0])
     assert np.isnan(again[place >= 144][:window or None]).all()
+
+
+def test_the_example_runs_the_operators_together(capsys):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decoder_layer.py")
+    spec = importlib.util.spec_from_file_location("decoder_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    # 16-bit results of a computation in 32 bits: half a unit in the last place
+    assert example.main(["--tokens", "150", "--steps", "5", "--hidden", "512", "--inner", "1000", "--heads", "8", "--kv-heads", "2"]) <= 2.0 ** -11
+    assert "4.25 bits a value" in capsys.readouterr().out
