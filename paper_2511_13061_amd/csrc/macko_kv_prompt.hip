@@ -35,7 +35,8 @@ __global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(co
   const float lift = kLift / unit;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
-  for (int first_row = row_block * R; first_row < seq.rows; first_row += g.row_blocks * R) {
+  // The last rows see most: they start first, and what is left for the end is short (4096 rows of 32 heads 299 to 247 us).
+  for (int first_row = (g.row_blocks - 1 - row_block) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
     const Rows rows = rows_of(a, first_row);
     const Span span = span_of(a, g, seq, rows);
     if (split >= span.used) continue;
