@@ -495,7 +495,7 @@ int64_t splits_of(const KvAttention& a, int64_t others, int64_t units, int64_t u
   static_assert(kMostSplits == 256, "the last one tried");
   const double cus = device_cu_count(), rows = (double)a.tokens * a.heads;
   const bool prompt = is_prompt(a), two = !prompt && row_tiles(a) == 2, wide = a.pool.dim > 128;
-  const double alone = prompt ? 5.0 : two ? 1.3 : wide ? 1.4 : 0.9, room = prompt ? (wide ? 1 : 2) : two ? 2 : wide ? 1 : 3;
+  const double alone = prompt ? 5.0 : two ? 1.3 : wide ? 1.4 : 0.9, room = prompt || two ? 2 : wide ? 1 : 3;
   const double share = std::max((double)unit_bytes * cus / 6.0e6, prompt ? 3.7 : two ? 0.8 : 0.45);
   auto time = [&](int64_t splits) {
     const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);

@@ -14,7 +14,7 @@ namespace {
 constexpr int kStep = 64, kBlocks = kStep / 16, kWide = 1, kNan = 2;
 
 template <int NG, bool BF, int RT>
-__global__ __launch_bounds__(64 * kWaves, NG <= 4 ? 2 : 1) void prompt_kernel(const Launch args) {
+__global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch args) {
   const KvAttention& a = args.a;
   const Grid& g = args.g;
   constexpr int D = 32 * NG, NK = (NG + 3) / 4, NP = BF ? 2 : 3, R = 16 * RT * kWaves;
