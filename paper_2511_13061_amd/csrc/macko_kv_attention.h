@@ -185,9 +185,13 @@ __device__ inline void parts_of(const float* w, V4i& hi, V4i& lo) {
   for (int i = 0; i < 4; ++i) {
     const float w0 = w[2 * i], w1 = w[2 * i + 1];
     if (HALF) {
-      const H2 h = {(_Float16)w0, (_Float16)w1}, l = {(_Float16)(w0 - (float)h[0]), (_Float16)(w1 - (float)h[1])};
-      hi[i] = __builtin_bit_cast(int, h);
-      lo[i] = __builtin_bit_cast(int, l);
+      // what is left over comes from the pair as it is packed: one instruction a weight that takes half of a register as it is and rounds what it gives
+      float less = -1.f;
+      asm("" : "+s"(less));                              // (a plain difference is made of three)
+      const int pair = later(__builtin_bit_cast(int, H2{(_Float16)w0, (_Float16)w1}));
+      const H2 h = __builtin_bit_cast(H2, pair);
+      hi[i] = pair;
+      lo[i] = __builtin_bit_cast(int, H2{(_Float16)__builtin_fmaf((float)h[0], less, w0), (_Float16)__builtin_fmaf((float)h[1], less, w1)});
     } else {
       // cut off, not rounded: that takes no instruction but the one that joins two of them
       const uint32_t b0 = __builtin_bit_cast(uint32_t, w0), b1 = __builtin_bit_cast(uint32_t, w1);

@@ -32,7 +32,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
   const uint8_t* const pool = a.pool.data + head * piece;
   const int page_size = 1 << a.pool.page_bits;
   const float unit = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f, sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
-  const float lift = kLift / unit;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
   // The last rows see most: they start first, and what is left for the end is short (4096 rows of 32 heads 299 to 247 us).
@@ -154,14 +153,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       if (lane < 16) lds_spoilt[(wave * RT + rt) * 16 + lane] = 0;
     }
 
-    float top[RT];
+    // Of a row: -(running maximum), and by how far a score may pass that, in powers of two; nothing seen yet: 0 and not at all.
+    float base[RT], limit[RT];
     V4f out[RT][2 * NG], total[RT];                      // the sum of the weights, the same in every row
     // All steps; true: not to be done this way.
     auto go = [&](auto half) {
       constexpr bool HALF = decltype(half)::value;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        top[rt] = -INFINITY;
+        base[rt] = 0.f;
+        limit[rt] = -INFINITY;
         total[rt] = V4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c) out[rt][c] = V4f{0.f, 0.f, 0.f, 0.f};
@@ -209,17 +210,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
             float x[8];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              V4f y = {0.f, 0.f, 0.f, 0.f};
+              V4f sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
               for (int kk = 0; kk < NK; ++kk) {
                 const V4i k4 = key[2 * s + u][kk];
                 const V8i k8 = {k4[0], k4[1], k4[2], k4[3], 0, 0, 0, 0};
-                if (NP == 3) y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NP - 1], y, 4, 0, 0, key_byte[2 * s + u][kk], 2, q_byte[rt][kk]);
-                y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][1], y, 4, 0, 0, key_byte[2 * s + u][kk], 1, q_byte[rt][kk]);
-                y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], y, 4, 0, 0, key_byte[2 * s + u][kk], 0, q_byte[rt][kk]);
+                if (NP == 3) sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NP - 1], sum, 4, 0, 0, key_byte[2 * s + u][kk], 2, q_byte[rt][kk]);
+                sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][1], sum, 4, 0, 0, key_byte[2 * s + u][kk], 1, q_byte[rt][kk]);
+                sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], sum, 4, 0, 0, key_byte[2 * s + u][kk], 0, q_byte[rt][kk]);
               }
 #pragma unroll
-              for (int i = 0; i < 4; ++i) x[4 * u + i] = y[i];
+              for (int i = 0; i < 4; ++i) x[4 * u + i] = sum[i];
             }
             if (s == 1 && rt == RT - 1) {                 // in the registers of this step's, and in those that the next one's values have left
               if (more) load_keys(at + kStep, slot + 1);
@@ -232,21 +233,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
                 if ((uint32_t)(place[rt] - token) >= reach) x[i] = -INFINITY;
               }
             }
-            const float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            if (__any(most > top[rt] + lift)) {
-              float to = fmaxf(most, __shfl_xor(most, 16));
-              to = fmaxf(to, __shfl_xor(to, 32));
-              to = fmaxf(to, top[rt]);
-              const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
-              top[rt] = to;
+            float y[8];                                   // against the running maximum as it was
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[i], unit, base[rt]);
+            const float most = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+            if (__any(most > limit[rt])) {
+              float by = fmaxf(most, __shfl_xor(most, 16));
+              by = fmaxf(by, __shfl_xor(by, 32));
+              if (limit[rt] == kLift) by = fmaxf(by, 0.f);
+              if (by > -INFINITY) {
+                const float to = base[rt] - by;
+                by = limit[rt] == kLift ? __builtin_amdgcn_exp2f(to - base[rt]) : 1.f;
+                base[rt] = to;
+                limit[rt] = kLift;
+              } else {
+                by = 1.f;
+              }
               total[rt] *= by;
 #pragma unroll
               for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
-            }
-            const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
-            parts_of<HALF>(x, p_hi[rt], p_lo[rt]);
+              for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[i], unit, base[rt]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_exp2f(y[i]);
+            parts_of<HALF>(y, p_hi[rt], p_lo[rt]);
           }
           constexpr bool ONE = HALF && BF;
           const int one = HALF ? 0x3C003C00 : 0x3F803F80;
@@ -261,10 +272,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
           for (int c = 0; c < 2 * NG; ++c) {
             const V4i v = from[c * 64];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-              if (!ONE) out[rt][c] = multiply<HALF>(v, p_lo[rt], out[rt][c]);
-              out[rt][c] = multiply<HALF>(v, p_hi[rt], out[rt][c]);
-            }
+            for (int rt = 0; rt < RT && !ONE; ++rt) out[rt][c] = multiply<HALF>(v, p_lo[rt], out[rt][c]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) out[rt][c] = multiply<HALF>(v, p_hi[rt], out[rt][c]);
           }
         }
         if (slot == 4) ahead = entry(at + 4 * kStep);
@@ -293,7 +303,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       if (row >= seq.rows) continue;
       const int query = rows.query_of(a, g, row), h = head * e->a.shared + row - query * e->a.shared;
       const int64_t token = seq.first + query;
-      const float sum = bad ? NAN : total[rt][0], most = top[rt] * unit;
+      const float sum = bad ? NAN : total[rt][0], most = limit[rt] == kLift ? -base[rt] : -INFINITY;
       const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
       const float r = span.used > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
       uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + quad * 4;
