@@ -27,8 +27,9 @@ struct Tile {
   uint32_t value[2][NG], value_byte[2][NG];      // [token of 4][g] bytes
 };
 
-// Wavefronts on a SIMD that the registers are to leave room for.
-constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? (ng <= 4 ? 2 : 1) : ng == 1 ? 4 : ng <= 4 ? 3 : 1; }
+// Wavefronts on a SIMD that the registers are to leave room for, as many as they can without spills.  Two for 160 and 192 channels a head: 3.3 to 5.2 and
+// 4.0 to 6.1 TB/s.
+constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? 2 : ng == 1 ? 4 : ng <= 4 ? 3 : ng <= 6 ? 2 : 1; }
 
 template <int NG, bool BF, int RT>
 __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_kernel(const Launch args) {
@@ -495,7 +496,7 @@ int64_t splits_of(const KvAttention& a, int64_t others, int64_t units, int64_t u
   static_assert(kMostSplits == 256, "the last one tried");
   const double cus = device_cu_count(), rows = (double)a.tokens * a.heads;
   const bool prompt = is_prompt(a), two = !prompt && row_tiles(a) == 2, wide = a.pool.dim > 128;
-  const double alone = prompt ? 5.0 : two ? 1.3 : wide ? 1.4 : 0.9, room = prompt || two ? 2 : wide ? 1 : 3;
+  const double alone = prompt ? 5.0 : two ? 1.3 : wide ? 1.4 : 0.9, room = prompt || two ? 2 : a.pool.dim > 192 ? 1 : wide ? 2 : 3;
   const double share = std::max((double)unit_bytes * cus / 6.0e6, prompt ? 3.7 : two ? 0.8 : 0.45);
   auto time = [&](int64_t splits) {
     const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);
