@@ -18,6 +18,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
   const KvAttention& a = args.a;
   const Grid& g = args.g;
   constexpr int D = 32 * NG, NK = (NG + 3) / 4, NP = BF ? 2 : 3, R = 16 * RT * kWaves;
+  constexpr int SHARE = NG <= 2 ? 4 / NG : 1, NI = (NP + SHARE - 1) / SHARE;      // parts of a query that one instruction takes; instructions
   extern __shared__ __align__(16) V4i lds[];             // [2][2][2 NG][64]: 8 tokens of one channel, for a step, 32 of its tokens, 16 channels and a lane
   uint32_t* const outside = reinterpret_cast<uint32_t*>(lds + 2 * 2 * 2 * NG * 64);     // [2][kWaves]: what look_over has found in a step's values
   uint32_t* const lds_spoilt = outside + 2 * kWaves;     // [kWaves][RT][16]: groups in which a row sees what is not a number
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
     const Rows rows = rows_of(a, first_row);
     const Span span = span_of(a, g, seq, rows);
     if (split >= span.used) continue;
-    const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4;
+    const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4, group = SHARE > 1 ? j % NG : j;
     const int begin = span.lo + split * span.chunk, end = span.hi - begin > span.chunk ? begin + span.chunk : span.hi;
     const int last_block = (end - 1) >> 4;
     bool bad = end > begin && (a.table_width == 0 || a.pool.pages == 0);
@@ -71,9 +72,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
         for (int kk = 0; kk < NK; ++kk) {
           key[u][kk] = V4i{0, 0, 0, 0};
           key_byte[u][kk] = 0;
-          if (kk * 4 + j < NG) {
-            key[u][kk] = *reinterpret_cast<const V4i*>(codes + (uint32_t)(n * (D / 2) + j * 16) + kk * 64);
-            key_byte[u][kk] = (codes + bytes)[(uint32_t)(n * NG + j) + kk * 4];
+          if (SHARE > 1 || kk * 4 + j < NG) {
+            key[u][kk] = *reinterpret_cast<const V4i*>(codes + (uint32_t)(n * (D / 2) + group * 16) + kk * 64);
+            key_byte[u][kk] = (codes + bytes)[(uint32_t)(n * NG + group) + kk * 4];
           }
         }
       }
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
 
     // the rows of this lane
     int place[RT];
-    V8i q[RT][NK][NP];
+    V8i q[RT][NK][NI];
     int q_byte[RT][NK];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -148,7 +149,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       const bool there = row < seq.rows;
       place[rt] = there ? seq.length - seq.queries + query : -1;
       const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
-      load_queries<NG, BF>(src, there, sign, n, j, q[rt], q_byte[rt]);
+      V8i part[NK][NP];
+      load_queries<NG, BF>(src, there, sign, n, j, part, q_byte[rt]);
+      if constexpr (SHARE == 1) {
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) q[rt][kk][p] = part[kk][p];
+      } else {
+        // Narrow heads leave room: an instruction takes the same keys against SHARE parts, channel 0 of part p at p D.
+        const uint32_t bytes = (uint32_t)__shfl(q_byte[rt][0], n + 16 * group);
+        const int p = j / NG;
+        q_byte[rt][0] = (int)((bytes >> 8 * min(p, NP - 1) & 255u) | (bytes >> 16 & 255u) << 8);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if (NG == 1) {
+            const int second = __shfl(part[0][1][w], lane & 31);
+            q[rt][0][0][w] = j < 2 ? part[0][0][w] : second;
+            q[rt][0][0][4 + w] = NP == 3 && j < 2 ? part[0][NP - 1][w] : 0;
+          } else {
+            q[rt][0][0][w] = part[0][0][w];
+            q[rt][0][0][4 + w] = part[0][1][w];
+            if (NP == 3) {
+              q[rt][0][NI - 1][w] = part[0][2 % NP][w];
+              q[rt][0][NI - 1][4 + w] = 0;
+            }
+          }
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);                  // one tile of rows at a time, or the registers do not hold what lies between
       if (lane < 16) lds_spoilt[(wave * RT + rt) * 16 + lane] = 0;
     }
@@ -215,8 +243,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
               for (int kk = 0; kk < NK; ++kk) {
                 const V4i k4 = key[2 * s + u][kk];
                 const V8i k8 = {k4[0], k4[1], k4[2], k4[3], 0, 0, 0, 0};
-                if (NP == 3) sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NP - 1], sum, 4, 0, 0, key_byte[2 * s + u][kk], 2, q_byte[rt][kk]);
-                sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][1], sum, 4, 0, 0, key_byte[2 * s + u][kk], 1, q_byte[rt][kk]);
+                if (NI == 3) sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NI - 1], sum, 4, 0, 0, key_byte[2 * s + u][kk], 2, q_byte[rt][kk]);
+                if (NI >= 2) sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][NI >= 2 ? 1 : 0], sum, 4, 0, 0, key_byte[2 * s + u][kk], 1, q_byte[rt][kk]);
                 sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], sum, 4, 0, 0, key_byte[2 * s + u][kk], 0, q_byte[rt][kk]);
               }
 #pragma unroll
