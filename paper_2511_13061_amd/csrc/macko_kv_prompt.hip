@@ -233,9 +233,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
 #pragma unroll
         for (int s = 0; s < 2; ++s) {                     // 32 tokens at a time: weights, then products
           V4i p_hi[RT], p_lo[RT];
+          float scores[RT][8];                            // of all tiles of rows first: the matrix cores are at the next one's while one is weighed
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
-            float x[8];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               V4f sum = {0.f, 0.f, 0.f, 0.f};
@@ -248,12 +248,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
                 sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, q[rt][kk][0], sum, 4, 0, 0, key_byte[2 * s + u][kk], 0, q_byte[rt][kk]);
               }
 #pragma unroll
-              for (int i = 0; i < 4; ++i) x[4 * u + i] = sum[i];
+              for (int i = 0; i < 4; ++i) scores[rt][4 * u + i] = sum[i];
             }
-            if (s == 1 && rt == RT - 1) {                 // in the registers of this step's, and in those that the next one's values have left
-              if (more) load_keys(at + kStep, slot + 1);
-              if (at + 2 * kStep < end) load_values(at + 2 * kStep, slot + 2);
-            }
+          }
+          if (s == 1) {                                   // in the registers of this step's, and in those that the next one's values have left
+            if (more) load_keys(at + kStep, slot + 1);
+            if (at + 2 * kStep < end) load_values(at + 2 * kStep, slot + 2);
+          }
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float(&x)[8] = scores[rt];
             if (at < span.all_lo || at + kStep > span.all_hi) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
