@@ -57,7 +57,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   const float lift = kLift / unit;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
-  for (int first_row = row_block * R; first_row < seq.rows; first_row += g.row_blocks * R) {
+  // the last rows see most and start first
+  for (int first_row = (g.row_blocks - 1 - row_block) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
     const Rows rows = rows_of(a, first_row);
     const Span span = span_of(a, g, seq, rows);
     if (split >= span.used) continue;
@@ -391,7 +392,8 @@ __device__ inline void write_joined(const KvAttention& a, int64_t id, int channe
   if (a.sums && channel == 0) a.sums[id] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
-// Few splits: a wavefront has a row, a lane the maximum and the sum of one split.
+// Few splits: a wavefront has a row, a lane the maximum and the sum of one split.  512 rows of 32 heads with 64 channels in 4 parts: 96 us with the attention,
+// 111 with a workgroup a row; with more parts a row's reads take longer than a wavefront's share is worth (8 rows in 32 parts 14.6 and 13.6).
 constexpr int kFewSplits = 16;
 template <int NG, bool BF>
 __global__ __launch_bounds__(256) void join_few_kernel(const KvAttention a, const Grid g) {
@@ -478,53 +480,70 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
   write_joined<BF>(a, id, channel, o, most, (total_of[0] + total_of[1]) + (total_of[2] + total_of[3]));
 }
 
-// Two tiles of rows share the decoded values where there are more rows than one has (beyond 128 channels the registers do not hold two).
+// Two tiles of rows share the decoded values where there are more rows than one has (beyond 128 channels the registers do not hold two): 32 rows on 16
+// sequences of 4096 tokens, 8 heads of 128 channels 32 us, 35 with one tile; 20 rows 30 and 32, 128 rows 72 and 99.
 int row_tiles(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > 16 && a.pool.dim <= 128 ? 2 : 1; }
-// Rows from which the kernel for many rows takes a call.
+// Rows up to which the kernel for many rows is not thought of: half of a workgroup's have none there (64 rows on 16 sequences of 4096 tokens, 8 heads of 128
+// channels: 73 us, 47 here).
 constexpr int kPromptRows = 64;
-bool is_prompt(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > kPromptRows; }
+// Rows of a workgroup
+int rows_of_block(const KvAttention& a, bool prompt) { return prompt ? 16 * kWaves * prompt_row_tiles(a.pool.dim) : 16 * row_tiles(a); }
+bool is_prompt(const Grid& g) { return g.rows >= 64; }
 
 constexpr int64_t kMostGrid = 65535;       // of a launch's second and third dimension
 
+struct Dealt {
+  int64_t splits;
+  double time;
+};
 // How many parts the tokens of a sequence are dealt out to: the number with the shortest estimate, in microseconds.  A workgroup goes on by 128 tokens (one
 // step of each wavefront, two for many rows) in the time that it takes alone, or that the workgroups of a compute unit take for one each where that is
-// longer: from memory (6 TB/s) or on the vector units.  Workgroups take turns where more of them come than fit, and each has 5 to begin and to end.  Joining costs
-// a launch, the sums' way through memory and something for each part.  Constants from 33 calls of 1 to 64 sequences of 256 to 131072 tokens, 1 to 512 queries, heads of 32 to 256
-// channels, with 1 to 128 parts each; the choice took 2 % longer than the best of these in the mean, 12 at worst.
-int64_t splits_of(const KvAttention& a, int64_t others, int64_t units, int64_t unit_bytes) {
+// longer: from memory (6 TB/s, once for all rows of a sequence) or on the vector units and matrix cores.  Workgroups take turns where more of them come than fit, and each has 5 to begin and
+// to end.  Joining costs a launch, the sums' way through memory and something for each part.  Constants from 75 calls of 1 to 64 sequences of 256 to 131072
+// tokens, 1 to 1024 queries, heads of 32 to 256 channels, with 1 to 128 parts each and, of 96 to 2048 rows, by both kernels; the choice of parts and kernel
+// took 2 % longer than the best of these in the mean, a quarter at worst (160 rows of 64 channels).  What it chooses for 16 sequences of 4096, 8 heads of 128
+// channels in bf16 (this kernel / the one for many rows): 128 rows 66 us (66 / 67), 256 rows 113 (124 / 112), 512 rows 172 (232 / 172).
+Dealt deal(const KvAttention& a, bool prompt, int64_t row_blocks, int64_t units, int64_t unit_bytes) {
   static constexpr int kTry[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
   static_assert(kMostSplits == 256, "the last one tried");
+  const int64_t others = (int64_t)a.batch * a.pool.heads * row_blocks;
   const double cus = device_cu_count(), rows = (double)a.tokens * a.heads;
-  const bool prompt = is_prompt(a), two = !prompt && row_tiles(a) == 2, wide = a.pool.dim > 128;
-  const double alone = prompt ? 5.0 : two ? 1.3 : wide ? 1.4 : 0.9, room = prompt || two ? 2 : a.pool.dim > 192 ? 1 : wide ? 2 : 3;
-  const double share = std::max((double)unit_bytes * cus / 6.0e6, prompt ? 3.7 : two ? 0.8 : 0.45);
+  const bool two = !prompt && row_tiles(a) == 2, wide = a.pool.dim > 128, narrow = a.pool.dim <= 64, one_part = prompt && a.type == MACKO_BF16;
+  const double alone = prompt ? (wide ? 6.4 : narrow ? 4.5 : 5.1) * (one_part ? 0.82 : 1.0) : two ? 1.3 : wide ? 1.4 : 0.9;
+  const double busy_share = prompt ? (narrow ? 2.2 : 3.2) * (one_part ? 0.82 : 1.0) : two ? (narrow ? 0.65 : 0.86) : wide ? 0.82 : 0.45;
+  const double room = prompt || two ? 2 : a.pool.dim > 192 ? 1 : wide ? 2 : 3, share = std::max((double)unit_bytes * cus / 6.0e6 / (double)row_blocks, busy_share);
   auto time = [&](int64_t splits) {
     const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);
     const double turns = groups <= 4.0 * room ? std::ceil(groups / room) : groups / room + 0.5;
     const double join = splits > 1 ? 3.4 + 0.02 * (double)splits + rows * (double)splits * (a.pool.dim + 2) * 8.0 / 4.0e6 : 0.0;
     return turns * (5.0 + steps * std::max(alone, busy * share)) + join;
   };
-  int64_t best = 1;
+  Dealt best{1, time(1)};
   if (a.tokens * a.heads >= int64_t{1} << 24) return best;      // a join has a workgroup a row, and a launch fewer than 2^32 threads
-  double least = time(1);
   for (const int splits : kTry) {
     if (splits > units) break;
     const double t = time(splits);
-    if (t < least) least = t, best = splits;
+    if (t < best.time) best = Dealt{splits, t};
   }
   return best;
 }
 
 Grid grid_of(const KvAttention& a) {
   Grid g{};
-  const bool prompt = is_prompt(a);
-  g.rows = prompt ? 16 * kWaves * prompt_row_tiles(a.pool.dim) : 16 * row_tiles(a);
   g.unit = kWaves * kTile;
-  const int64_t row_blocks = ((int64_t)a.most_queries * a.shared + g.rows - 1) / g.rows;
   g.shared_inverse = a.shared == 1 ? 0u : (uint32_t)(((uint64_t{1} << 32) + a.shared - 1) / a.shared);
-  const int64_t others = (int64_t)a.batch * a.pool.heads * row_blocks, unit = g.unit;
+  const int64_t unit = g.unit, most_rows = (int64_t)a.most_queries * a.shared;
   const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
-  const int64_t splits = splits_of(a, others, (longest + unit - 1) / unit, kv_piece_bytes(unit, a.pool.dim));
+  auto blocks_of = [&](bool prompt) { return (most_rows + rows_of_block(a, prompt) - 1) / rows_of_block(a, prompt); };
+  auto dealt = [&](bool prompt) { return deal(a, prompt, std::max<int64_t>(1, blocks_of(prompt)), (longest + unit - 1) / unit, kv_piece_bytes(unit, a.pool.dim)); };
+  Dealt dealt_out = dealt(false);
+  bool prompt = false;
+  if (most_rows > kPromptRows) {
+    const Dealt as_prompt = dealt(true);
+    if (as_prompt.time < dealt_out.time) dealt_out = as_prompt, prompt = true;
+  }
+  const int64_t splits = dealt_out.splits, row_blocks = blocks_of(prompt), others = (int64_t)a.batch * a.pool.heads * row_blocks;
+  g.rows = rows_of_block(a, prompt);
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
   g.splits = (int32_t)((longest + g.chunk - 1) / g.chunk);
   g.row_blocks = (int32_t)std::min(row_blocks, kMostGrid / g.splits);      // of a launch: a workgroup goes on to others
@@ -545,7 +564,7 @@ template <int NG, bool BF>
 int launch_type(const KvAttention& a, const Grid& g, hipStream_t stream) {
   int status = MACKO_OK;
   bool one = true;
-  if (is_prompt(a)) {
+  if (is_prompt(g)) {
     status = launch_prompt(a, g, stream);
     one = false;
   } else if constexpr (NG <= 4) {

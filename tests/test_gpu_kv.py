@@ -681,3 +681,60 @@ def test_the_example_runs_the_operators_together(capsys):
     # 16-bit results of a computation in 32 bits: half a unit in the last place
     assert example.main(["--tokens", "150", "--steps", "5", "--hidden", "512", "--inner", "1000", "--heads", "8", "--kv-heads", "2"]) <= 2.0 ** -11
     assert "4.25 bits a value" in capsys.readouterr().out
+
+
+# A call's parts and its kernel follow an estimate of the time, which goes by the rows that there may be: with room for very many it is the kernel for
+# many rows, without splits; with the room of the second test, with splits.
+def attend_with_room(attend, cache, q, tables, lengths, tokens, **more):
+    """As attend(q, ...), with queries of no sequence behind those of q."""
+    wide = q.new_zeros((max(tokens, q.shape[0]), *q.shape[1:]))
+    wide[:q.shape[0]] = q
+    got = attend(cache, wide, tables, lengths, **dict(more, most_queries=wide.shape[0]))
+    return tuple(x[:q.shape[0]] for x in got) if isinstance(got, tuple) else got[:q.shape[0]]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(PROMPT)))
+def test_attention_of_many_rows_by_the_kernel_for_them(case, dtype):
+    dim, page, heads, kv_heads, lengths, queries, window = PROMPT[case]
+    g = rng(2000 + case)
+    cache = pool(g, sum(-(-n // page) for n in lengths) + 2, page, kv_heads, dim)
+    tables = sequences(g, cache, lengths)
+    fill(g, cache, tables, lengths)
+    start = np.concatenate([[0], np.cumsum(queries)])
+    q = normal(g, sum(queries), heads, dim, dtype=dtype, scale=1.5)
+    want = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, lengths, start, window=window)
+    got, sums = attend_with_room(M.KvCache.attend, cache, q.cuda(), ints(tables), ints(lengths), 2 ** 18 // heads, start=ints(start), window=window, sums=True)
+    check_attention(got, sums, *want, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,room", [(256, 512), (128, 1024), (64, 1024)])
+def test_attention_of_many_rows_in_parts(dim, room, dtype):
+    g = rng(2100 + dim)
+    page, lengths, queries = 64, [8001, 0, 17, 1, 0, 700, 64, 0], [90, 3, 17, 1, 0, 130, 2, 0]
+    cache = pool(g, 150, page, 1, dim)
+    tables = sequences(g, cache, lengths)
+    fill(g, cache, tables, lengths)
+    start = np.concatenate([[0], np.cumsum(queries)])
+    q = normal(g, sum(queries), 1, dim, dtype=dtype)
+    want = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, lengths, start)
+    got, sums = attend_with_room(M.KvCache.attend, cache, q.cuda(), ints(tables), ints(lengths), room, start=ints(start), longest=max(lengths), sums=True)
+    check_attention(got, sums, *want, dtype)
+
+
+@pytest.fixture
+def very_many(monkeypatch):
+    attend = M.KvCache.attend
+    monkeypatch.setattr(M.KvCache, "attend", lambda self, q, tables, lengths, **more: attend_with_room(attend, self, q, tables, lengths, 2 ** 18 // q.shape[1], **more))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [(1e-4,), (2e-7, 1.0), (1.0, 3e4), (1e-6,), (0.0, 1.0), (0.0,), (1e-6, 1e4, 0.0)])
+def test_attention_of_many_rows_values_of_any_size(very_many, sizes, dtype):
+    test_attention_values_of_any_size(sizes, 90, dtype)
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_what_is_masked_has_no_effect_in_the_kernel_for_many_rows(very_many, window):
+    test_attention_of_many_rows_what_is_masked_has_no_effect(window)
