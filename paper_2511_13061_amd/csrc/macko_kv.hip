@@ -107,6 +107,8 @@ __device__ inline uint32_t turn_bytes(uint32_t word, int lane) {
   return __builtin_amdgcn_perm(far, word, lane & 8 ? 0x03020706u : 0x05040100u);
 }
 
+// Memory bounds it: 8191 tokens of 40 heads with 128 channels, normalised and turned, 33 us (5.1 TB/s; a copy reaches 4.8 to 5.2); 16384 tokens of 32 heads into
+// the cache, q, k and v, 74 us.  One token takes 3 us, a launch's own time.
 // Queries, keys and values have workgroups of their own.  A group of lanes takes BUNDLE heads of a token, whose loads are under way together;
 // position, table row and weight serve all of them.
 template <bool BF, int BUNDLE>
@@ -267,6 +269,7 @@ __device__ inline Packed8 decode8(uint32_t word, uint32_t byte) {
   return {decode2<BF, 0>(word, unit), decode2<BF, 1>(word, unit), decode2<BF, 2>(word, unit), decode2<BF, 3>(word, unit)};
 }
 
+// Memory bounds it, and it writes four fifths of what it moves: 65536 slots of 8 heads with 128 channels 52 us, 6.4 TB/s (writing alone reaches 6.9).
 template <bool BF, int BUNDLE>
 __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
   const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1), groups = kBlock >> a.lane_bits, n = a.pool.dim / 32;
