@@ -30,15 +30,18 @@ struct Tile {
   uint32_t value[2][NG], value_byte[2][NG];      // [token of 4][g] bytes
 };
 
-// Wavefronts on a SIMD that the registers are to leave room for, as many as they can without spills.  Two for 160 and 192 channels a head: 3.3 to 5.2 and
-// 4.0 to 6.1 TB/s.
-constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? 2 : ng == 1 ? 4 : ng <= 4 ? 3 : ng <= 6 ? 2 : 1; }
+// Wavefronts on a SIMD that the registers are to leave room for, as many as they can without spills (several parts of a query in an instruction made room for
+// one more of narrow heads).  Two for 160 and 192 channels a head: 3.3 to 5.2 and 4.0 to 6.1 TB/s.
+constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? (ng == 1 ? 4 : ng == 2 ? 3 : 2) : ng <= 2 ? 4 : ng <= 4 ? 3 : ng <= 6 ? 2 : 1; }
 
 template <int NG, bool BF, int RT>
 __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_kernel(const Launch args) {
   const KvAttention& a = args.a;
   const Grid& g = args.g;
   constexpr int D = 32 * NG, NK = (NG + 3) / 4, NP = BF ? 2 : 3, R = 16 * RT, LD = D + 4;
+  // Narrow heads leave room in an instruction: it takes the same keys against SHARE parts of a query, channel 0 of part p at p D (64 sequences of up
+  // to 4096 tokens, 32 heads of 64 channels 135 to 127 us, 64 rows on 64 of 2048 61 to 54).
+  constexpr int SHARE = NG <= 2 ? 4 / NG : 1, NI = (NP + SHARE - 1) / SHARE;
   extern __shared__ __align__(16) float lds[];           // [kWaves][16][LD], maxima and sums [kWaves][16] each, and below
   float* const lds_max = lds + kWaves * 16 * LD;
   float* const lds_sum = lds_max + kWaves * 16;
@@ -83,7 +86,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       bad = bad || __any(!fine);
       pages = fine ? page : 0;
     };
-    const uint32_t key_lane = n * (D / 2) + j * 16, key_byte_lane = n * NG + j, value_lane = (j * 16 + n) * (4 * NG), value_byte_lane = j * (4 * NG);
+    const int key_group = SHARE > 1 ? j % NG : j;
+    const uint32_t key_lane = n * (D / 2) + key_group * 16, key_byte_lane = n * NG + key_group, value_lane = (j * 16 + n) * (4 * NG), value_byte_lane = j * (4 * NG);
     auto load = [&](Tile<NG>& t, int at, int slot) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -92,7 +96,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
         const uint8_t* const bytes = codes + page_size * D - in_page * (D / 2 - NG);
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-          const int group = kk * 4 + j;
+          const int group = kk * 4 + key_group;
           t.key[u][kk] = V4i{0, 0, 0, 0};
           t.key_byte[u][kk] = 0;
           if (group < NG) {
@@ -122,7 +126,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
       for (int rt = 0; rt < RT; ++rt) lds_spoilt[(rt * kWaves + wave) * 16 + lane] = 0;
     }
     int place[RT];                                        // of a row's query: it sees the tokens t with 0 <= place - t < reach
-    V8i q[RT][NK][NP];
+    V8i q[RT][NK][NI];
     int q_byte[RT][NK];
     // The queries' operand (load_queries says what it is), 8 channels of a row by each thread, through LDS to the lanes of all wavefronts.
     constexpr int kChunks = R * 4 * NG, kTurns = (kChunks + 64 * kWaves - 1) / (64 * kWaves);
@@ -161,21 +165,38 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
     for (int rt = 0; rt < RT; ++rt) {
       const int row = first_row + rt * 16 + n;
       place[rt] = row < seq.rows ? seq.length - seq.queries + rows.query_of(a, g, row) : -1;
+      if constexpr (SHARE > 1) {
+        auto part_at = [&](int p, int lane_of) { return *reinterpret_cast<const V4i*>(lds_q + ((rt * NP + p) * 64 + lane_of) * 8); };
+        const int t = lds_byte[(rt * 16 + n) * NG + key_group];
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
+        for (int i = 0; i < NI; ++i) {
+          // part by group of lanes: the low half of the operand has channels 16 j of it, the high half 64 on
+          const int p = i * SHARE + (NG == 1 ? j >> 1 : 0), p_high = NG == 1 ? 2 + (j >> 1) : i * SHARE + 1, from = NG == 1 ? (j & 1) * 16 + n : lane;
+          const V4i low = part_at(min(p, NP - 1), from), high = part_at(min(p_high, NP - 1), from);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const V4i* const from = reinterpret_cast<const V4i*>(lds_q + (((rt * NK + kk) * NP + p) * 64 + lane) * 8);
-          V4i half[2] = {from[0], from[1]};
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            if (NG % 4 != 0 && kk * 128 + u * 64 + j * 16 >= D) half[u] = V4i{0, 0, 0, 0};      // no such channels
-#pragma unroll
-            for (int w = 0; w < 4; ++w) q[rt][kk][p][u * 4 + w] = half[u][w];
+          for (int w = 0; w < 4; ++w) {
+            q[rt][0][i][w] = p < NP ? low[w] : 0;
+            q[rt][0][i][4 + w] = p_high < NP ? high[w] : 0;
           }
         }
-        const int t = kk * 4 + j < NG ? lds_byte[(rt * 16 + n) * NG + kk * 4 + j] : 20;
-        q_byte[rt][kk] = t | (t - 4) << 8 | (t - 8) << 16;
+        q_byte[rt][0] = (t - 4 * min(j / NG, NP - 1)) | (t - 8) << 8;
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const V4i* const from = reinterpret_cast<const V4i*>(lds_q + (((rt * NK + kk) * NP + p) * 64 + lane) * 8);
+            V4i half[2] = {from[0], from[1]};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              if (NG % 4 != 0 && kk * 128 + u * 64 + j * 16 >= D) half[u] = V4i{0, 0, 0, 0};      // no such channels
+#pragma unroll
+              for (int w = 0; w < 4; ++w) q[rt][kk][p][u * 4 + w] = half[u][w];
+            }
+          }
+          const int t = kk * 4 + j < NG ? lds_byte[(rt * 16 + n) * NG + kk * 4 + j] : 20;
+          q_byte[rt][kk] = t | (t - 4) << 8 | (t - 8) << 16;
+        }
       }
     }
 
@@ -191,8 +212,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
 #pragma unroll
           for (int kk = 0; kk < NK; ++kk) {
             const V8i key = {t.key[u][kk][0], t.key[u][kk][1], t.key[u][kk][2], t.key[u][kk][3], 0, 0, 0, 0};
-            if (NP == 3) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q[rt][kk][NP - 1], s, 4, 0, 0, t.key_byte[u][kk], 2, q_byte[rt][kk]);
-            s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q[rt][kk][1], s, 4, 0, 0, t.key_byte[u][kk], 1, q_byte[rt][kk]);
+            if (NI == 3) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q[rt][kk][NI - 1], s, 4, 0, 0, t.key_byte[u][kk], 2, q_byte[rt][kk]);
+            if (NI >= 2) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q[rt][kk][NI >= 2 ? 1 : 0], s, 4, 0, 0, t.key_byte[u][kk], 1, q_byte[rt][kk]);
             s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q[rt][kk][0], s, 4, 0, 0, t.key_byte[u][kk], 0, q_byte[rt][kk]);
           }
 #pragma unroll
@@ -504,7 +525,7 @@ struct Dealt {
 // longer: from memory (6 TB/s, once for all rows of a sequence) or on the vector units and matrix cores.  Workgroups take turns where more of them come than fit, and each has 5 to begin and
 // to end.  Joining costs a launch, the sums' way through memory and something for each part.  Constants from 75 calls of 1 to 64 sequences of 256 to 131072
 // tokens, 1 to 1024 queries, heads of 32 to 256 channels, with 1 to 128 parts each and, of 96 to 2048 rows, by both kernels; the choice of parts and kernel
-// took 2 % longer than the best of these in the mean, a quarter at worst (160 rows of 64 channels).  What it chooses for 16 sequences of 4096, 8 heads of 128
+// took 2 % longer than the best of these in the mean, 14 % at worst.  What it chooses for 16 sequences of 4096, 8 heads of 128
 // channels in bf16 (this kernel / the one for many rows): 128 rows 66 us (66 / 67), 256 rows 113 (124 / 112), 512 rows 172 (232 / 172).
 Dealt deal(const KvAttention& a, bool prompt, int64_t row_blocks, int64_t units, int64_t unit_bytes) {
   static constexpr int kTry[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
@@ -514,7 +535,7 @@ Dealt deal(const KvAttention& a, bool prompt, int64_t row_blocks, int64_t units,
   const bool two = !prompt && row_tiles(a) == 2, wide = a.pool.dim > 128, narrow = a.pool.dim <= 64, one_part = prompt && a.type == MACKO_BF16;
   const double alone = prompt ? (wide ? 6.4 : narrow ? 4.5 : 5.1) * (one_part ? 0.82 : 1.0) : two ? 1.3 : wide ? 1.4 : 0.9;
   const double busy_share = prompt ? (narrow ? 2.2 : 3.2) * (one_part ? 0.82 : 1.0) : two ? (narrow ? 0.65 : 0.86) : wide ? 0.82 : 0.45;
-  const double room = prompt || two ? 2 : a.pool.dim > 192 ? 1 : wide ? 2 : 3, share = std::max((double)unit_bytes * cus / 6.0e6 / (double)row_blocks, busy_share);
+  const double room = two && narrow ? 3 : prompt || two ? 2 : a.pool.dim > 192 ? 1 : wide ? 2 : 3, share = std::max((double)unit_bytes * cus / 6.0e6 / (double)row_blocks, busy_share);
   auto time = [&](int64_t splits) {
     const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);
     const double turns = groups <= 4.0 * room ? std::ceil(groups / room) : groups / room + 0.5;
