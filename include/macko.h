@@ -474,7 +474,8 @@ MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const
  * tokens t <= p, with a window > 0 only those with t > p - window.  Head h reads
  * key/value head h / (heads / kv_heads).
  *   out = sum over seen t of softmax(scale * q.k_t) v_t,   sums = log sum exp(scale * q.k_t)
- * A query that sees nothing gets zeros and a sum of -infinity.  What lies in
+ * A query that sees nothing gets zeros and a sum of -infinity.  A weight goes into its products with 16 bits, whatever its size; calls of many queries in
+ * bf16 without sums_dev may take 11 bits, where no row's results are off by more than half a unit in the last place of its largest for that.  What lies in
  * tokens that a query does not see, in the rest of pages and in table entries that no
  * query of the sequence needs has no effect on it, NaN included (values that other
  * queries see may decide how a query's own are multiplied, and change its last place).  A table entry that a

@@ -2,8 +2,10 @@
 // step, not memory.  The four wavefronts of a workgroup have rows of their own and go along the tokens together, 64 at a time:
 //   values   are decoded once for all of them, a quarter by each, into LDS, as the operand of the matrix instruction: a lane's 8 tokens of one
 //            channel lie together.  The steps are staggered: while step t is multiplied, t + 1 is decoded and t + 2 is on its way from memory.
-//            In fp16, which holds factors from 2^-19 to 2^12 exactly; a workgroup that meets another one starts again and takes bf16.
-//   weights  are one fp16 part (11 bits) for results in bf16, two for fp16; two parts of their type with values in bf16.
+//            In bf16, which holds them exactly; for results in bf16 alone in fp16, which does so for factors from 2^-19 to 2^12.
+//   weights  are two bf16 parts (16 bits).  For results in bf16 alone, whose sums nobody asks for, they are one fp16 part: 11 bits from 2^-24 of a row's
+//            maximum on, and below that 2^-35 of it at most too much or too little.  Rows for which that may be too coarse, and factors beyond fp16, are found
+//            behind the steps, and their block is done again in bf16.  One fp16 part takes 303 us where two bf16 parts take 386 (the case below).
 //   scores   as in macko_kv_attention.hip: keys as they lie in memory.
 //   sums     of the weights come from the matrix cores too (a row of ones).
 // 64 tokens, because their keys and a step's scores are what the registers hold of two tiles of rows for two wavefronts on a SIMD; that is what hides one
@@ -18,9 +20,15 @@ namespace macko {
 namespace {
 
 constexpr int kStep = 64, kBlocks = kStep / 16, kWide = 1, kNan = 2;
+// Weights in fp16, which goes from 2^-24 to 2^16: the running maximum is at 2^10, and a weight may be 2^5 times that before it moves (2^12 and 2^3: up to 4 % slower).
+constexpr float kHalfTop = 10.f, kHalfLift = 5.f;
+constexpr float kHalfFar = 0x1.8p14f;                     // the largest value that goes to fp16
+
+// Wavefronts on a SIMD: 64 channels leave room for a third (4096 queries of 2 sequences, bf16: 211 us, 280 with two).
+constexpr int prompt_waves(int ng, bool bf) { return ng == 2 && bf ? 3 : 2; }
 
 template <int NG, bool BF, int RT>
-__global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch args) {
+__global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kernel(const Launch args) {
   const KvAttention& a = args.a;
   const Grid& g = args.g;
   constexpr int D = 32 * NG, NK = (NG + 3) / 4, NP = BF ? 2 : 3, R = 16 * RT * kWaves;
@@ -41,11 +49,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
   const float unit = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f, sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
+  bool in_half = BF && !a.sums;                           // the way that a block of rows is done in
   // The last rows see most: they start first, and what is left for the end is short (4096 rows of 32 heads 299 to 247 us).
-  for (int first_row = (g.row_blocks - 1 - row_block) * R; first_row < seq.rows; first_row += g.row_blocks * R) {
+  for (int first_row = (g.row_blocks - 1 - row_block) * R; first_row < seq.rows;) {
     const Rows rows = rows_of(a, first_row);
     const Span span = span_of(a, g, seq, rows);
-    if (split >= span.used) continue;
+    if (split >= span.used) {
+      first_row += g.row_blocks * R;
+      continue;
+    }
     const int lane = later(threadIdx.x) & 63, n = lane & 15, j = lane >> 4, group = SHARE > 1 ? j % NG : j;
     const int begin = span.lo + split * span.chunk, end = span.hi - begin > span.chunk ? begin + span.chunk : span.hi;
     const int last_block = (end - 1) >> 4;
@@ -187,12 +199,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       if (lane < 16) lds_spoilt[(wave * RT + rt) * 16 + lane] = 0;
     }
 
-    // Of a row: -(running maximum), and by how far a score may pass that, in powers of two; nothing seen yet: 0 and not at all.
+    // Of a row: what its scores are lifted by, and how large they may then be, in powers of two; nothing seen yet: 0 and -infinity.
     float base[RT], limit[RT];
     V4f out[RT][2 * NG], total[RT];                      // the sum of the weights, the same in every row
-    // All steps; true: not to be done this way.
+    // All steps; true: in fp16, which did not hold all values.
     auto go = [&](auto half) {
       constexpr bool HALF = decltype(half)::value;
+      constexpr float kTop = HALF ? kHalfTop : 0.f, kMost = kTop + (HALF ? kHalfLift : kLift);      // where the running maximum is put, and where it moves
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         base[rt] = 0.f;
@@ -209,7 +222,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       look_over(begin, 0);
       __syncthreads();
       int now = found(0);
-      if (HALF && (now & kWide)) return true;
+      int all = now;
       decode(begin, 0, now, half);
       load_values(begin + kStep, 1);
       look_over(begin + kStep, 1);
@@ -218,7 +231,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       for (int at = begin, parity = 0, slot = 0; at < end; at += kStep, parity ^= 1) {
         const bool more = at + kStep < end;
         const int next = more ? found(parity ^ 1) : 0;
-        if (HALF && (next & kWide)) return true;
+        all |= next;
         if (more) decode(at + kStep, parity ^ 1, next, half);
         if (now & kNan) {                                 // values that are not numbers have been left out: the rows that see them are marked
 #pragma unroll 1
@@ -278,12 +291,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
             if (__any(most > limit[rt])) {
               float by = fmaxf(most, __shfl_xor(most, 16));
               by = fmaxf(by, __shfl_xor(by, 32));
-              if (limit[rt] == kLift) by = fmaxf(by, 0.f);
+              if (limit[rt] > -INFINITY) by = fmaxf(by, kTop);
               if (by > -INFINITY) {
-                const float to = base[rt] - by;
-                by = limit[rt] == kLift ? __builtin_amdgcn_exp2f(to - base[rt]) : 1.f;
+                const float to = base[rt] - (by - kTop);
+                by = limit[rt] > -INFINITY ? __builtin_amdgcn_exp2f(to - base[rt]) : 1.f;
                 base[rt] = to;
-                limit[rt] = kLift;
+                limit[rt] = kMost;
               } else {
                 by = 1.f;
               }
@@ -324,10 +337,62 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
         }
         __syncthreads();
       }
-      return false;
+      return HALF && (all & kWide);
     };
-    if (go(std::integral_constant<bool, true>{})) {
-      __syncthreads();
+    if (BF && in_half) {
+      const bool wide = go(std::integral_constant<bool, BF>{});
+      float least = wide ? -1.f : INFINITY;               // the largest result of a row that sees something, of the row where that is smallest
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float large = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2 * NG; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) large = fmaxf(large, fabsf(out[rt][c][i]));
+        large = fmaxf(large, __shfl_xor(large, 16));
+        large = fmaxf(large, __shfl_xor(large, 32));
+        if (total[rt][0] > 0.f) least = fminf(least, large);
+      }
+      // A weight below fp16's normal numbers is off by 2^-25 at most.  Whether that, with no value larger than `far`, may come to more than half a unit in the
+      // last place of a row's largest result, in any wavefront.
+      auto left_out = [&](float far) {
+        const bool much = __any(least < (float)(end - begin) * far * 0x1p-25f * 0x1p9f);
+        if (lane == 0) outside[wave] = much;
+        __syncthreads();
+        return found(0) != 0;
+      };
+      // The largest magnitude that a value of [span.first, end) can have by the factors of all groups.
+      auto largest_value = [&] {
+        uint32_t top = 0;
+#pragma unroll 1
+        for (int block = (begin >> 4) + wave * 64 + lane; block <= last_block; block += 64 * kWaves) {
+          const int index = block >> (a.pool.page_bits - 4), page = table[min(index, a.table_width - 1)];
+          const uint8_t* const piece_of = pool + (index < a.table_width && page >= 0 && page < a.pool.pages ? page : 0) * page_stride;
+          const V4i* const vb = reinterpret_cast<const V4i*>(piece_of + page_size * (D + NG) + ((block << 4) & (page_size - 1)) * NG);
+#pragma unroll 1
+          for (int w = 0; w < NG; ++w) {
+            const V4i word = vb[w];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const uint32_t byte = (uint32_t)word[k >> 2] >> 8 * (k & 3) & 255u;
+              const int token = (block << 4) + (w * 16 + k) / NG;
+              if (token >= span.first && token < end && byte < 255u) top = max(top, byte);
+            }
+          }
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        if (lane == 0) outside[kWaves + wave] = top;
+        __syncthreads();
+        const uint32_t* const o = outside + kWaves;
+        return 6.f * __builtin_bit_cast(float, max(max(o[0], o[1]), max(o[2], o[3])) << 23);
+      };
+      if (left_out(kHalfFar) && (wide || left_out(largest_value()))) {
+        in_half = false;
+        __syncthreads();
+        continue;
+      }
+    } else {
       go(std::integral_constant<bool, false>{});
     }
 
@@ -341,7 +406,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       if (row >= seq.rows) continue;
       const int query = rows.query_of(a, g, row), h = head * e->a.shared + row - query * e->a.shared;
       const int64_t token = seq.first + query;
-      const float sum = bad ? NAN : total[rt][0], most = limit[rt] == kLift ? -base[rt] : -INFINITY;
+      const float sum = bad ? NAN : total[rt][0], most = limit[rt] > -INFINITY ? -base[rt] : -INFINITY;
       const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
       const float r = span.used > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
       uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + quad * 4;
@@ -368,6 +433,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(const Launch arg
       if (e->g.splits > 1) used_splits(e->a, e->g)[token * e->a.heads + h] = 1;
       if (e->a.sums) e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
+    in_half = BF && !a.sums;
+    first_row += g.row_blocks * R;
     __syncthreads();                                      // the marks are cleared for the next rows
   }
 }
