@@ -47,7 +47,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   float* const lds_sum = lds_max + kWaves * 16;
   uint32_t* const lds_spoilt = reinterpret_cast<uint32_t*>(lds_sum + kWaves * 16);      // [RT][kWaves][16]: groups in which a row sees what is not a number
   uint32_t* const lds_q = lds_spoilt + RT * kWaves * 16;                                // [RT][NK][NP][64][8]
-  uint8_t* const lds_byte = reinterpret_cast<uint8_t*>(lds_q + RT * NK * NP * 512);     // [R][NG]
+  // [RT][thread]: a lane's sum up to the last 32 steps, out of the registers' way.  A token that is far ahead of very many others would lose them, step by step.
+  float* const lds_whole = reinterpret_cast<float*>(lds_q + RT * NK * NP * 512);
+  uint8_t* const lds_byte = reinterpret_cast<uint8_t*>(lds_whole + RT * 64 * kWaves);   // [R][NG]
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x, split = g.splits == 1 ? 0 : g.row_blocks == 1 ? (int)blockIdx.z : (int)blockIdx.z / g.row_blocks, row_block = (int)blockIdx.z - split * g.row_blocks;
@@ -76,6 +78,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
     const int last_block = (end - 1) >> 4;
     float top[RT], sum[RT];
     V4f out[RT][2 * NG];
+    auto gather = [&] {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        lds_whole[rt * 64 * kWaves + later(threadIdx.x)] += sum[rt];
+        sum[rt] = 0.f;
+      }
+    };
 
     // A lane holds the page of one block of the wavefront's next 32 steps: one load for all of them, ahead of the loads that need it.
     int pages = 0;
@@ -234,16 +243,15 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
           top[rt] = to;
           sum[rt] *= by;
+          lds_whole[rt * 64 * kWaves + later(threadIdx.x)] *= by;
 #pragma unroll
           for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
         }
         const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;       // nothing seen yet: weights of 2^-inf, not NaN
         float weight[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
-          sum[rt] += weight[i];
-        }
+        for (int i = 0; i < 8; ++i) weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
+        sum[rt] += ((weight[0] + weight[1]) + (weight[2] + weight[3])) + ((weight[4] + weight[5]) + (weight[6] + weight[7]));
         parts_of<false>(weight, p_hi[rt], p_lo[rt]);
       }
       if (careful || at + kTile > seq.length) {
@@ -298,7 +306,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         top[rt] = -INFINITY;
-        sum[rt] = 0.f;
+        sum[rt] = lds_whole[rt * 64 * kWaves + later(threadIdx.x)] = 0.f;
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c) out[rt][c] = V4f{0.f, 0.f, 0.f, 0.f};
       }
@@ -313,6 +321,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           if (++slot == 32) {
             look_up(next);
             slot = 0;
+            gather();
           }
           load(t, next, slot);
         };
@@ -349,6 +358,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
     const int thread = later(threadIdx.x), row16 = thread & 15, quad = thread >> 4 & 3;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
+      sum[rt] += lds_whole[rt * 64 * kWaves + thread];
       sum[rt] += __shfl_xor(sum[rt], 16);
       sum[rt] += __shfl_xor(sum[rt], 32);
       if (bad) sum[rt] = NAN;
@@ -577,7 +587,7 @@ Grid grid_of(const KvAttention& a) {
 
 template <int NG, bool BF, int RT>
 int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
-  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + (2 + RT) * kWaves * 16 + RT * ((NG + 3) / 4) * (BF ? 2 : 3) * 512) + 16 * RT * NG;
+  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + (2 + RT) * kWaves * 16 + RT * ((NG + 3) / 4) * (BF ? 2 : 3) * 512 + RT * 64 * kWaves) + 16 * RT * NG;
   if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<NG, BF, RT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   hipLaunchKernelGGL((attention_kernel<NG, BF, RT>), dim3((unsigned)a.pool.heads, (unsigned)a.batch, (unsigned)(g.row_blocks * g.splits)), dim3(64 * kWaves), lds, stream, Launch{a, g});
   MACKO_HIP_TRY(hipGetLastError());

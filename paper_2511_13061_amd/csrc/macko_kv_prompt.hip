@@ -7,7 +7,7 @@
 //            maximum on, and below that 2^-35 of it at most too much or too little.  Rows for which that may be too coarse, and factors beyond fp16, are found
 //            behind the steps, and their block is done again in bf16.  One fp16 part takes 303 us where two bf16 parts take 386 (the case below).
 //   scores   as in macko_kv_attention.hip: keys as they lie in memory.
-//   sums     of the weights come from the matrix cores too (a row of ones).
+//   sums     of the weights come from the matrix cores too (a row of ones), 512 tokens at a time; those are added up with what rounding leaves out.
 // 64 tokens, because their keys and a step's scores are what the registers hold of two tiles of rows for two wavefronts on a SIMD; that is what hides one
 // wavefront's softmax behind another's products, as far as it is hidden.  1024 queries on each of 2 sequences of 8192 tokens, 32 heads on 8 of 128 channels, bf16:
 // 303 us, 850 TFLOP/s of the 1340 to 1373 that a product of 8192 x 8192 matrices reaches.  Of the 5700 cycles of a step on a SIMD the matrix cores are busy for
@@ -201,7 +201,18 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
 
     // Of a row: what its scores are lifted by, and how large they may then be, in powers of two; nothing seen yet: 0 and -infinity.
     float base[RT], limit[RT];
-    V4f out[RT][2 * NG], total[RT];                      // the sum of the weights, the same in every row
+    V4f out[RT][2 * NG], total[RT];                      // the sum of the weights since it last went into `whole`, the same in every row
+    // The sum up to there and what its roundings left out: a token that is far ahead of very many others would lose them, step by step.
+    float whole[RT], rest[RT];
+    auto gather = [&] {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float more = total[rt][0], sum = whole[rt] + more, by = sum - whole[rt];
+        rest[rt] += (whole[rt] - (sum - by)) + (more - by);
+        whole[rt] = sum;
+        total[rt] = V4f{0.f, 0.f, 0.f, 0.f};
+      }
+    };
     // All steps; true: in fp16, which did not hold all values.
     auto go = [&](auto half) {
       constexpr bool HALF = decltype(half)::value;
@@ -210,6 +221,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
       for (int rt = 0; rt < RT; ++rt) {
         base[rt] = 0.f;
         limit[rt] = -INFINITY;
+        whole[rt] = rest[rt] = 0.f;
         total[rt] = V4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c) out[rt][c] = V4f{0.f, 0.f, 0.f, 0.f};
@@ -301,6 +313,8 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
                 by = 1.f;
               }
               total[rt] *= by;
+              whole[rt] *= by;
+              rest[rt] *= by;
 #pragma unroll
               for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
 #pragma unroll
@@ -334,9 +348,11 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
         if (++slot == 8) {
           take(at + kStep, ahead);
           slot = 0;
+          gather();
         }
         __syncthreads();
       }
+      gather();
       return HALF && (all & kWide);
     };
     if (BF && in_half) {
@@ -351,7 +367,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
           for (int i = 0; i < 4; ++i) large = fmaxf(large, fabsf(out[rt][c][i]));
         large = fmaxf(large, __shfl_xor(large, 16));
         large = fmaxf(large, __shfl_xor(large, 32));
-        if (total[rt][0] > 0.f) least = fminf(least, large);
+        if (whole[rt] > 0.f) least = fminf(least, large);
       }
       // A weight below fp16's normal numbers is off by 2^-25 at most.  Whether that, with no value larger than `far`, may come to more than half a unit in the
       // last place of a row's largest result, in any wavefront.
@@ -406,7 +422,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
       if (row >= seq.rows) continue;
       const int query = rows.query_of(a, g, row), h = head * e->a.shared + row - query * e->a.shared;
       const int64_t token = seq.first + query;
-      const float sum = bad ? NAN : total[rt][0], most = limit[rt] > -INFINITY ? -base[rt] : -INFINITY;
+      const float sum = bad ? NAN : whole[rt] + rest[rt], most = limit[rt] > -INFINITY ? -base[rt] : -INFINITY;
       const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
       const float r = span.used > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
       uint16_t* const dst = reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + quad * 4;

@@ -68,3 +68,13 @@ def test_attention_one_token_ahead_of_many(tokens, gap, kernel, dtype, sums):
     for (i, h), (first, w, p, seen) in rows.items():
         want = w * seen / (1 + w * p)
         assert np.linalg.norm(got[i, h] - want) <= (HALF[dtype] + off_of(first)) * np.linalg.norm(want) + TINY[dtype] * len(want) ** 0.5, (i, h)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("tokens,gap", GAPS)
+def test_attention_sums_of_one_token_ahead_of_many(tokens, gap, kernel, dtype):
+    """The others' weights are too small to be added to the first one's alone; what they come to together is not."""
+    _, sums, rows = one_ahead_of_many(tokens, gap, kernel, dtype, True)
+    for (i, h), (first, w, p, _) in rows.items():
+        assert abs(sums[i, h] - (first + math.log1p(w * p))) <= first * 2.0 ** -21 + off_of(first) * w * p / (1 + w * p) + 2.0 ** -20, (i, h)
