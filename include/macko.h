@@ -378,7 +378,9 @@ MACKO_API int macko_dense_gemv_group(int n, const void* const* W_dev, const int6
  * and one of 0, .5, 1, 1.5, 2, 3, 4, 6.  b is the least one that brings the
  * largest magnitude to 7 times the factor at most; codes are rounded to nearest,
  * ties to the even code, and stop at 6.  A group that holds an infinity or a NaN
- * has b = 255 and reads as NaN.
+ * has b = 255 and reads as NaN.  Values of 2^128 and more, which b = 253 and 254 can
+ * stand for, read as infinities; what macko_kv_attention gives for a query that sees a
+ * value group with such a b is not defined (for others it has no effect, as NaN).
  *
  * 16-bit tensors are fp16 or bf16 (`type`), the same for all of a call; element
  * d of head h of token t lies at [t * ..._token + h * ..._head + d], strides in

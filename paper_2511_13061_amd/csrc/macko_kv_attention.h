@@ -17,6 +17,7 @@ typedef _Float16 H8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4, kTile = 32, kMostSplits = 256;
 constexpr int kMostTokens = 1 << 30;                  // of a sequence: sums of a length and a launch's steps stay in 31 bits
+constexpr uint32_t kNoNumber = 253; // a group of values with this byte or a higher one may read as infinite in bf16 and in 32 bits, with 255 it is NaN
 constexpr float kLift = 8.f;       // how far, in powers of two, a score may pass the running maximum before that moves
 
 struct Grid {

@@ -255,8 +255,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
         parts_of<false>(weight, p_hi[rt], p_lo[rt]);
       }
       if (careful || at + kTile > seq.length) {
-        // Tokens behind the sequence's end may hold anything: their factor becomes the least one.  In a careful pass that of values that are
-        // not numbers does too, and rows that see them are marked.
+        // Tokens behind the sequence's end may hold anything: their factor becomes the least one.  In a careful pass that of values that may
+        // not be numbers does too, and rows that see them are marked.
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
             for (int i = 0; i < NG; ++i) {
               const int byte = k * NG + i, shift = 8 * (byte & 3);
               uint32_t& word = t.value_byte[u][byte >> 2];
-              const bool nan = (word >> shift & 255u) == 255u && token < seq.length;
+              const bool nan = (word >> shift & 255u) >= kNoNumber && token < seq.length;
               if (token >= seq.length || (careful && nan)) word &= ~(255u << shift);
               if (careful && nan) {
 #pragma unroll
@@ -336,9 +336,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           if (at >= end) break;
         }
       }
-      // A value that is not a number reaches every row of its tile, with weight 0 where it is not seen: then the tokens are gone through
-      // again, carefully.  Nothing but such values gets here.
-      float all[4] = {0.f, 0.f, 0.f, 0.f};                // infinities of both signs make one too: that costs time alone
+      // A value that is not a number, or infinite, reaches every row of its tile, with weight 0 where it is not seen: then the tokens are gone
+      // through again, carefully.  (A row's own NaN, of its query or a key that it sees, gets here too, and costs time alone.)
+      float all[4] = {0.f, 0.f, 0.f, 0.f};                // infinities of both signs make one too: time alone
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll

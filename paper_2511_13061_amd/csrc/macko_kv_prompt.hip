@@ -109,7 +109,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
       }
     };
     // What there is to see to in the wavefront's values of a step, of tokens that a row may see: kWide, factors beyond 2^-19 to 2^12 (bytes 108 to 139; 0 is
-    // a group of zeros), kNan, values that are not numbers.
+    // a group of zeros), kNan, values that may not be numbers.
     auto look_over = [&](int at, int parity) {
       uint32_t far = 0;                                   // each byte 0 to 31 once 108 is taken off (one below borrows, and shows that itself)
 #pragma unroll
@@ -122,8 +122,8 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
           const uint32_t byte = value_byte[k >> 2] >> 8 * (k & 3) & 255u;
           const int token = at + wave * 16 + j * 4 + k / NG;
           const bool counts = token >= span.first && token < end;
-          nan = nan || (counts && byte == 255u);
-          wide = wide || (counts && byte != 255u && byte > 139u) || (counts && byte < 108u && byte != 0u);
+          nan = nan || (counts && byte >= kNoNumber);
+          wide = wide || (counts && byte < kNoNumber && byte > 139u) || (counts && byte < 108u && byte != 0u);
         }
         what = (__any(wide) ? kWide : 0) | (__any(nan) ? kNan : 0);
       }
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
 #pragma unroll
           for (int i = 0; i < NG; ++i) {
             const int byte = k * NG + i, shift = 8 * (byte & 3);
-            if (token < span.first || token >= end || (value_byte[byte >> 2] >> shift & 255u) == 255u) value_byte[byte >> 2] &= ~(255u << shift);
+            if (token < span.first || token >= end || (value_byte[byte >> 2] >> shift & 255u) >= kNoNumber) value_byte[byte >> 2] &= ~(255u << shift);
           }
         }
       }
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
 #pragma unroll 1
             for (int k = 0; k < 4 * NG; ++k) {
               const int token = at + u * 16 + j * 4 + k / NG;
-              if (vb[k] != 255 || token >= end) continue;
+              if (vb[k] < kNoNumber || token >= end) continue;
 #pragma unroll
               for (int rt = 0; rt < RT; ++rt)
                 if ((uint32_t)(place[rt] - token) < reach) atomicOr(lds_spoilt + (wave * RT + rt) * 16 + n, 1u << k % NG);
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * kWaves, prompt_waves(NG, BF)) void prompt_kern
             for (int k = 0; k < 16; ++k) {
               const uint32_t byte = (uint32_t)word[k >> 2] >> 8 * (k & 3) & 255u;
               const int token = (block << 4) + (w * 16 + k) / NG;
-              if (token >= span.first && token < end && byte < 255u) top = max(top, byte);
+              if (token >= span.first && token < end && byte < kNoNumber) top = max(top, byte);
             }
           }
         }

@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 import kv_reference as ref
-from test_gpu_kv import HALF, TINY, TYPES, attend_with_room, ints, normal, pool, rng, sequences
+from test_gpu_kv import HALF, TINY, TYPES, attend_with_room, fill, ints, normal, pool, rng, sequences
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,44 @@ def test_attention_sums_of_one_token_ahead_of_many(tokens, gap, kernel, dtype):
     _, sums, rows = one_ahead_of_many(tokens, gap, kernel, dtype, True)
     for (i, h), (first, w, p, _) in rows.items():
         assert abs(sums[i, h] - (first + math.log1p(w * p))) <= first * 2.0 ** -21 + off_of(first) * w * p / (1 + w * p) + 2.0 ** -20, (i, h)
+
+
+# ---- what is not seen ----------------------------------------------------------
+
+def spoil(cache, tables, tokens, byte):
+    """Values of these tokens of sequence 0 get the largest code, of both signs, and this byte in every group."""
+    page, dim = cache.page_size, cache.head_dim
+    data = cache.data.cpu().numpy()
+    for t in tokens:
+        _, (codes, _), _, groups = ref.addresses(page, dim, t % page, np.arange(dim))
+        data[tables[0, t // page]][:, codes], data[tables[0, t // page]][:, groups] = 0xF7, byte
+    cache.data.copy_(torch.from_numpy(data))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("kernel", ["few", "many"])
+@pytest.mark.parametrize("byte", [252, 253, 254, 255])
+@pytest.mark.parametrize("dim", [64, 160])
+def test_attention_values_beyond_the_range_have_no_effect_where_they_are_not_seen(dim, byte, kernel, window, dtype):
+    """Values of 2^128 and more, infinities in 32 bits, in tokens that some rows see and others do not."""
+    page, heads, kv_heads, length, asked = 16, 4, 2, 200, 120
+    clean, dirty = (pool(rng(1), 16, page, kv_heads, dim) for _ in range(2))
+    tables = sequences(rng(2), clean, [length])
+    for c in (clean, dirty):
+        fill(rng(9), c, tables, [length])
+    q = normal(rng(3), asked, heads, dim, dtype=dtype)
+    call = dict(start=ints([0, asked]), most_queries=asked, window=window, sums=True)
+    ask = lambda c: attend_with_room(M.KvCache.attend, c, q.cuda(), ints(tables), ints([length]), KERNELS[kernel][0], **call)  # noqa: E731
+    if kernel == "few":                                          # 8 queries with 2 heads of a cache head are one tile of rows
+        call.update(start=ints([0, 8]), most_queries=8)
+    first = length - (8 if kernel == "few" else asked)
+    want, total = ask(clean)
+    spots = (195, 130 if window else 198)
+    spoil(dirty, tables, spots, byte)
+    got, sums = ask(dirty)
+    place = np.arange(first, length)
+    free = [i for i, p in enumerate(place) if not any(t <= p and (not window or t > p - window) for t in spots)]
+    assert 2 < len(free) < len(place)
+    assert torch.equal(got[free], want[free]) and torch.equal(sums[free], total[free])
+    assert torch.isfinite(got[free]).all()
