@@ -376,10 +376,11 @@ MACKO_API int macko_dense_gemv_group(int n, const void* const* W_dev, const int6
  * 4.25 bits a value (OCP microscaling format MXFP4): 32 channels of one token and
  * head share a byte b, a factor 2^(b-127); each has a 4-bit code, a sign (bit 3)
  * and one of 0, .5, 1, 1.5, 2, 3, 4, 6.  b is the least one that brings the
- * largest magnitude to 7 times the factor at most; codes are rounded to nearest,
- * ties to the even code, and stop at 6.  A group that holds an infinity or a NaN
- * has b = 255 and reads as NaN.  Values of 2^128 and more, which b = 253 and 254 can
- * stand for, read as infinities; what macko_kv_attention gives for a query that sees a
+ * largest magnitude to 7 times the factor at most, and 252 at most, so that a number
+ * is never stored as an infinity; codes are rounded to nearest, ties to the even
+ * code, and stop at 6.  A group that holds an infinity or a NaN has b = 255 and reads
+ * as NaN.  b = 253 and 254 in a pool from elsewhere can stand for values of 2^128 and
+ * more, which read as infinities; what macko_kv_attention gives for a query that sees a
  * value group with such a b is not defined (for others it has no effect, as NaN).
  *
  * 16-bit tensors are fp16 or bf16 (`type`), the same for all of a call; element
@@ -476,6 +477,7 @@ MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const
  * tokens t <= p, with a window > 0 only those with t > p - window.  Head h reads
  * key/value head h / (heads / kv_heads).
  *   out = sum over seen t of softmax(scale * q.k_t) v_t,   sums = log sum exp(scale * q.k_t)
+ * The sum is divided last: where it passes 2^128 on the way (weights go up to 2^8 there), results are infinite.
  * A query that sees nothing gets zeros and a sum of -infinity.  A weight goes into its products with 16 bits, whatever its size; calls of many queries in
  * bf16 without sums_dev may take 11 bits, where no row's results are off by more than half a unit in the last place of its largest for that.  What lies in
  * tokens that a query does not see, in the rest of pages and in table entries that no

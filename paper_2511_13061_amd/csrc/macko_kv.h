@@ -14,6 +14,8 @@
 
 namespace macko {
 
+constexpr uint32_t kMostByte = 252;      // that a group of numbers is stored with: 6 * 2^125 is a number in bf16 and in 32 bits, 4 * 2^126 is not
+
 struct KvPool {
   uint8_t* data;
   int64_t pages;

@@ -72,7 +72,7 @@ __device__ inline uint32_t encode8(const float* y, uint32_t* byte) {
   bits = max(bits, dpp<kSwap2>(bits));
   // the exponent of most / 7, rounded up: 7 = 1.75 * 2^2, and a mantissa above 1.75 carries
   const uint32_t e = (bits + 0x1FFFFFu) >> 23;
-  const uint32_t b = bits >= 0x7F800000u ? 255u : e > 2u ? e - 2u : 0u;
+  const uint32_t b = bits >= 0x7F800000u ? 255u : e > 2u ? min(e - 2u, kMostByte) : 0u;
   *byte = b;
   const float unit = __builtin_bit_cast(float, b << 23);
   uint32_t word = 0;

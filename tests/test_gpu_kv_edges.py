@@ -119,3 +119,30 @@ def test_attention_values_beyond_the_range_have_no_effect_where_they_are_not_see
     assert 2 < len(free) < len(place)
     assert torch.equal(got[free], want[free]) and torch.equal(sums[free], total[free])
     assert torch.isfinite(got[free]).all()
+
+
+# ---- the largest numbers -------------------------------------------------------
+
+def test_the_largest_numbers_of_bf16_stay_numbers():
+    """6 * 2^125 is the largest number that the cache holds: what is above is stored as that, not as 2^128, which is an infinity."""
+    big = torch.finfo(torch.bfloat16).max
+    x = torch.zeros((5, 1, 64), dtype=torch.float64)
+    x[0, 0, :4] = torch.tensor([big, -big, 2.99e38, 2.0 ** 126])
+    x[1, 0, :3] = torch.tensor([1.75 * 2.0 ** 127, -2.0 ** 127, 2.0 ** 124])      # 7 * 2^125, to the nearest of 6 and 8: as far as b = 252 goes
+    x[2, 0, :2] = torch.tensor([1.5 * 2.0 ** 127, 2.0 ** 127])
+    x[3, 0, 0], x[3, 0, 33] = float("inf"), big
+    x[4, 0, 5] = -float("nan")
+    x = x.bfloat16()
+    cache = pool(rng(1), 1, 16, 1, 64)
+    cache.append(None, x.cuda(), x.cuda(), None, ints(np.arange(5)))
+    unit = 2.0 ** 125
+    want = np.zeros((5, 64))
+    want[0, :4] = 6 * unit, -6 * unit, 6 * unit, 2 * unit
+    want[1, :3] = 6 * unit, -4 * unit, 0.5 * unit
+    want[2, :2] = 6 * unit, 4 * unit
+    want[3, :32], want[3, 33], want[4, :32] = np.nan, 6 * unit, np.nan
+    for got in ref.read(cache.data.cpu().numpy(), 16, 64, np.arange(5)) + [ref.to_numpy(t) for t in cache.read(ints(np.arange(5)), torch.bfloat16)]:
+        assert np.array_equal(got[:, 0], want, equal_nan=True)
+    # a query that sees one token gets its values
+    q = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    assert np.array_equal(ref.to_numpy(cache.attend(q, ints([[0]]), ints([1])))[0, 0], want[0])
