@@ -431,8 +431,10 @@ int attention_of(const macko_kv_cache_t* cache, const macko_kv_attention_args_t*
         (g->table_width > 0 && !g->tables_dev) || !aligned_to(g->tables_dev, 4) || !aligned_to(g->start_dev, 4) || !aligned_to(g->sums_dev, 4))
       return MACKO_E_INVALID_ARG;
   }
+  // A sequence has 2^30 tokens at most: a window as long is none.  A longer one, taken off a place before the first token, would not fit 32 bits.
+  const int32_t window = g->window >= int32_t{1} << 30 ? 0 : g->window;
   *a = KvAttention{pool, static_cast<const uint8_t*>(g->q_dev), static_cast<uint8_t*>(g->out_dev), g->sums_dev, g->q_token, g->q_head, g->out_token, g->out_head,
-                   g->tables_dev, g->table_stride, g->lengths_dev, g->start_dev, g->table_width, g->batch, g->heads, g->heads / pool.heads, g->window, g->scale,
+                   g->tables_dev, g->table_stride, g->lengths_dev, g->start_dev, g->table_width, g->batch, g->heads, g->heads / pool.heads, window, g->scale,
                    (int32_t)std::max<int64_t>(1, std::min<int64_t>(g->most_queries, g->tokens)), g->tokens, g->longest, g->type};
   return kv_attention_fits(*a) ? MACKO_OK : MACKO_E_UNSUPPORTED;
 }

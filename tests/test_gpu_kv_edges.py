@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 import kv_reference as ref
-from test_gpu_kv import HALF, TINY, TYPES, attend_with_room, fill, ints, normal, pool, rng, sequences
+from test_gpu_kv import HALF, TINY, TYPES, attend_with_room, check_attention, fill, ints, normal, pool, rng, sequences
 
 pytestmark = pytest.mark.gpu
 
@@ -119,6 +119,22 @@ def test_attention_values_beyond_the_range_have_no_effect_where_they_are_not_see
     assert 2 < len(free) < len(place)
     assert torch.equal(got[free], want[free]) and torch.equal(sums[free], total[free])
     assert torch.isfinite(got[free]).all()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 60, 2 ** 30, 2 ** 30 - 1])
+@pytest.mark.parametrize("kernel", ["few", "many"])
+@pytest.mark.parametrize("length,asked", [(57, 60), (200, 300), (1, 90), (0, 5)])
+def test_attention_a_window_that_is_longer_than_any_sequence(length, asked, kernel, window):
+    """It hides nothing, of queries before the first token's place (there are more queries than tokens) either."""
+    page, dim = 16, 64
+    cache = pool(rng(1), 14, page, 1, dim)
+    tables = sequences(rng(2), cache, [length])
+    fill(rng(9), cache, tables, [length])
+    q = normal(rng(3), asked, 1, dim)
+    got, sums = attend_with_room(M.KvCache.attend, cache, q.cuda(), ints(tables), ints([length]), 2 * KERNELS[kernel][0], start=ints([0, asked]), most_queries=asked,
+                                 window=window, sums=True)
+    want, total, reach, far = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, [length], [0, asked])
+    check_attention(got, sums, want, total, reach, far, torch.float16)
 
 
 # ---- the largest numbers -------------------------------------------------------
