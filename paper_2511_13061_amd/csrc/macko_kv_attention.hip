@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
   const int page_size = 1 << a.pool.page_bits;
   // Weights are 2^(score * unit - maximum); the scale's sign goes into the queries, so that the largest score has the largest weight.
   const float unit = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f, sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
-  const float lift = kLift / unit;
+  const float lift = fminf(kLift / unit, 0x1p127f);      // finite: nothing is above -infinity by an infinity, and the first maximum would never be taken
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
   // the last rows see most and start first

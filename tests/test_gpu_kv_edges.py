@@ -80,6 +80,21 @@ def test_attention_sums_of_one_token_ahead_of_many(tokens, gap, kernel, dtype):
         assert abs(sums[i, h] - (first + math.log1p(w * p))) <= first * 2.0 ** -21 + off_of(first) * w * p / (1 + w * p) + 2.0 ** -20, (i, h)
 
 
+@pytest.mark.parametrize("scale", [1e-30, -1e-37, 1e-38, -2e-39, 1e-45])
+@pytest.mark.parametrize("kernel", ["few", "many"])
+def test_attention_of_scores_that_are_next_to_nothing(kernel, scale):
+    page, dim, length = 16, 64, 300
+    cache = pool(rng(1), 20, page, 2, dim)
+    tables = sequences(rng(2), cache, [length])
+    fill(rng(9), cache, tables, [length])
+    q = normal(rng(3), 1, 4, dim)
+    got, sums = attend_with_room(M.KvCache.attend, cache, q.cuda(), ints(tables), ints([length]), KERNELS[kernel][0] // 2, start=ints([0, 1]), most_queries=1,
+                                 scale=scale, sums=True)
+    want, total, reach, far = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, [length], [0, 1], scale=scale)
+    check_attention(got, sums, want, total, reach, far, torch.float16)
+    assert np.abs(total - math.log(length)).max() < 1e-20
+
+
 # ---- what is not seen ----------------------------------------------------------
 
 def spoil(cache, tables, tokens, byte):
