@@ -114,11 +114,11 @@ def _rotation(x, positions, table, interleaved, eps) -> _CRotation:
 
 
 @contextlib.contextmanager
-def _on(x, stream):
-    """Allocations of the call belong to the stream that it runs on; x must be on the current device, whose streams these are."""
+def _on(device, stream):
+    """Allocations of the call belong to the stream that it runs on; its tensors must be on the current device, whose streams these are."""
     torch = _need_torch()
-    if x.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {x.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
     if stream is None:
         yield
         return
@@ -132,8 +132,11 @@ def rope_table(length, rot, base=10000.0, first=0, factor=1.0, trained=0, low=1.
     factor > 1 scales for contexts longer than the `trained` length: frequencies that turn more than `high` times within it stay, those
     below `low` are divided by the factor, others are blended; with trained = 0 all are divided."""
     torch = _need_torch()
-    table = torch.empty((max(int(length), 0), 2, max(int(rot), 0) // 2), dtype=torch.float32, device=device)
-    with _on(table, stream):
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    with _on(device, stream):
+        table = torch.empty((max(int(length), 0), 2, max(int(rot), 0) // 2), dtype=torch.float32, device=device)
         _check(load_library().macko_rope_table(int(first), int(length), int(rot), base, factor, trained, low, high, amplitude,
                                                _dev_ptr(table), _stream_ptr(stream)), "macko_rope_table")
     return table
@@ -152,7 +155,7 @@ def rotate(x, positions, table, weight=None, eps=1e-6, interleaved=False, out=No
     src = _heads(x, "x", x.shape)
     r = _rotation(x, positions, table, interleaved, eps)
     w = _weight(weight, "weight", x)
-    with _on(x, stream):
+    with _on(x.device, stream):
         if out is None:
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         dst = _made_heads(out, "out", x.shape, x)
@@ -199,7 +202,7 @@ class KvCache:
         a.slots = _ints(slots, "slots", (tokens,), k)
         a.k_weight = _weight(k_weight, "k_weight", k)
         a.rotation = _rotation(k, positions, table, interleaved, eps)
-        with _on(k, stream):
+        with _on(k.device, stream):
             if q is not None:
                 shape = (tokens, q.shape[1] if q.dim() == 3 else 0, self.head_dim)
                 a.heads = shape[1]
@@ -222,7 +225,7 @@ class KvCache:
             if pair is not None:
                 return _made(pair, "macko_kv_read")
         shape = (slots.shape[0], self.kv_heads, self.head_dim)
-        with _on(self.data, stream):
+        with _on(self.data.device, stream):
             made = [torch.empty(shape, dtype=dtype, device=self.data.device) if x is None else x for x in (k_out, v_out)]
             if made[0].dtype != dtype:
                 raise ValueError("k_out and v_out must be of the type that is asked for")
@@ -264,7 +267,7 @@ class KvCache:
         a.longest = a.table_width * self.page_size if longest is None else int(longest)
         a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
         lib = load_library()
-        with _on(q, stream):
+        with _on(q.device, stream):
             if out is None:
                 out = torch.empty(shape, dtype=q.dtype, device=q.device)
             a.out, a.out_token, a.out_head = _made_heads(out, "out", shape, q)

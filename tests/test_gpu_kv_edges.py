@@ -177,3 +177,28 @@ def test_the_largest_numbers_of_bf16_stay_numbers():
     # a query that sees one token gets its values
     q = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
     assert np.array_equal(ref.to_numpy(cache.attend(q, ints([[0]]), ints([1])))[0, 0], want[0])
+
+
+# ---- the calls -----------------------------------------------------------------
+
+def test_results_are_allocated_on_the_stream_that_the_call_runs_on(monkeypatch):
+    """Memory of another stream's may still be in use there."""
+    side, empty, seen = torch.cuda.Stream(), torch.empty, []
+
+    def noted(*args, **more):
+        seen.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **more)
+
+    cache = M.KvCache(2, 16, 1, 64)
+    tab, x, at, slots, tables = M.rope_table(8, 64), torch.zeros((1, 1, 64), dtype=torch.float16, device="cuda"), ints([0]), ints([1]), ints([[0]])
+    calls = [lambda: M.rope_table(40, 64, stream=side), lambda: M.rope_table(40, 64, device="cuda:0", stream=side.cuda_stream), lambda: M.rotate(x, at, tab, stream=side),
+             lambda: cache.append(x, x, x, at, slots, tab, stream=side), lambda: cache.read(slots, stream=side), lambda: cache.attend(x, tables, ints([2]), sums=True, stream=side)]
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", noted)
+    for i, call in enumerate(calls):
+        seen.clear()
+        call()
+        assert seen and all(s == side.cuda_stream for s in seen), i
+    side.synchronize()
+    with pytest.raises(ValueError):
+        M.rope_table(4, 64, device="cpu")
