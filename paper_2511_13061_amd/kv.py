@@ -212,7 +212,7 @@ class KvCache:
                     q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
                 a.q_out, a.q_out_token, a.q_out_head = _made_heads(q_out, "q_out", shape, q)
             _check(load_library().macko_kv_append(self._p, ctypes.byref(a), _stream_ptr(stream)), "macko_kv_append")
-        return q_out
+        return q_out if q is not None else None
 
     def read(self, slots, dtype=None, k_out=None, v_out=None, stream=None):
         """macko_kv_read: keys and values [tokens, kv_heads, head_dim] of the slots (int32, below 0: zeros), in dtype (float16 by default)."""

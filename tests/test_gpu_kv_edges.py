@@ -202,3 +202,14 @@ def test_results_are_allocated_on_the_stream_that_the_call_runs_on(monkeypatch):
     side.synchronize()
     with pytest.raises(ValueError):
         M.rope_table(4, 64, device="cpu")
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_append_without_queries_returns_nothing(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(M.binding, "_native", None)
+    cache = M.KvCache(2, 16, 1, 64)
+    x = torch.ones((2, 1, 64), dtype=torch.float16, device="cuda")
+    assert cache.append(None, x, x, None, ints([0, 1])) is None
+    kept = torch.full_like(x, 3.0)
+    assert cache.append(None, x, x, None, ints([0, 1]), q_out=kept) is None and (kept == 3).all()
