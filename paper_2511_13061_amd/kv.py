@@ -92,6 +92,14 @@ def _ints(x, name, shape, like):
     return x.data_ptr()
 
 
+def _whole(value, name, bits=32):
+    """A whole number as the C interface takes it; ctypes would cut off what does not fit."""
+    value = int(value)
+    if not -2 ** (bits - 1) <= value < 2 ** (bits - 1):
+        raise ValueError(f"{name} = {value} does not fit {bits} bits")
+    return value
+
+
 def _weight(w, name, like):
     if w is None:
         return None
@@ -132,12 +140,13 @@ def rope_table(length, rot, base=10000.0, first=0, factor=1.0, trained=0, low=1.
     factor > 1 scales for contexts longer than the `trained` length: frequencies that turn more than `high` times within it stay, those
     below `low` are divided by the factor, others are blended; with trained = 0 all are divided."""
     torch = _need_torch()
+    length, rot, first = _whole(length, "length", 64), _whole(rot, "rot"), _whole(first, "first", 64)
     device = torch.device(device)
     if device.type == "cuda" and device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
     with _on(device, stream):
-        table = torch.empty((max(int(length), 0), 2, max(int(rot), 0) // 2), dtype=torch.float32, device=device)
-        _check(load_library().macko_rope_table(int(first), int(length), int(rot), base, factor, trained, low, high, amplitude,
+        table = torch.empty((max(length, 0), 2, max(rot, 0) // 2), dtype=torch.float32, device=device)
+        _check(load_library().macko_rope_table(first, length, rot, base, factor, trained, low, high, amplitude,
                                                _dev_ptr(table), _stream_ptr(stream)), "macko_rope_table")
     return table
 
@@ -170,7 +179,7 @@ class KvCache:
 
     def __init__(self, pages, page_size, kv_heads, head_dim, data=None, device="cuda"):
         torch = _need_torch()
-        c = _CCache(None, int(pages), int(page_size), int(kv_heads), int(head_dim))
+        c = _CCache(None, _whole(pages, "pages", 64), _whole(page_size, "page_size"), _whole(kv_heads, "kv_heads"), _whole(head_dim, "head_dim"))
         size = load_library().macko_kv_cache_bytes(ctypes.byref(c))
         if size < 0:
             _check(int(size), "macko_kv_cache_bytes")
@@ -263,8 +272,8 @@ class KvCache:
             a.start = _ints(start, "start", (batch + 1,), q)
         elif batch != shape[0]:
             raise ValueError("without start, q has one row a sequence")
-        a.most_queries, a.window = int(most_queries), int(window)
-        a.longest = a.table_width * self.page_size if longest is None else int(longest)
+        a.most_queries, a.window = _whole(most_queries, "most_queries"), _whole(window, "window")
+        a.longest = a.table_width * self.page_size if longest is None else _whole(longest, "longest", 64)
         a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
         lib = load_library()
         with _on(q.device, stream):

@@ -213,3 +213,17 @@ def test_append_without_queries_returns_nothing(native, monkeypatch):
     assert cache.append(None, x, x, None, ints([0, 1])) is None
     kept = torch.full_like(x, 3.0)
     assert cache.append(None, x, x, None, ints([0, 1]), q_out=kept) is None and (kept == 3).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_numbers_that_do_not_fit_the_interface_are_refused(native, monkeypatch):
+    """2^32 + 5 was a window of 5."""
+    if not native:
+        monkeypatch.setattr(M.binding, "_native", None)
+    cache = M.KvCache(4, 16, 1, 64)
+    cache.data.zero_()
+    q, tables, lengths = torch.zeros((1, 1, 64), dtype=torch.float16, device="cuda"), ints([[0, 1]]), ints([20])
+    for more in (dict(window=2 ** 32 + 5), dict(window=2 ** 31), dict(most_queries=2 ** 32 + 1), dict(most_queries=2 ** 31), dict(window=-1), dict(longest=-1)):
+        with pytest.raises((ValueError, M.MackoError)):
+            cache.attend(q, tables, lengths, **more)
+    assert (cache.attend(q, tables, lengths, window=2 ** 31 - 1, most_queries=2 ** 31 - 1, longest=2 ** 31 - 1) == 0).all()
