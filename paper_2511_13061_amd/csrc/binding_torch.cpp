@@ -314,7 +314,7 @@ PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
   a.type = type_of(*q.t);
   if (a.type < 0 || tokens == 0 || heads > INT32_MAX || batch > INT32_MAX || width > INT32_MAX || most < 1 || most > INT32_MAX || window < 0 || window > INT32_MAX ||
       longest < (args[7] == Py_None ? -1 : 0) || !heads_fit(*q.t, tokens, heads, dim, scalar, device) || !ints_fit(*lengths.t, batch, device) || tables.t->size(0) != batch ||
-      tables.t->scalar_type() != at::kInt || tables.t->stride(1) != 1 || !on(*tables.t, device) || (start.t ? !ints_fit(*start.t, batch + 1, device) : batch != tokens) ||
+      tables.t->scalar_type() != at::kInt || (width > 1 && tables.t->stride(1) != 1) || !on(*tables.t, device) || (start.t ? !ints_fit(*start.t, batch + 1, device) : batch != tokens) ||
       (out.t && !made_fits(*out.t, tokens, heads, dim, scalar, device)))
     Py_RETURN_NONE;
   a.tokens = tokens, a.heads = (int32_t)heads, a.batch = (int32_t)batch;

@@ -87,7 +87,7 @@ def _ints(x, name, shape, like):
         raise TypeError(f"{name} must be int32, not {x.dtype}")
     if tuple(x.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)}, not {list(x.shape)}")
-    if x.device != like.device or (x.numel() > 1 and x.stride(-1) != 1):
+    if x.device != like.device or (x.numel() > 1 and x.shape[-1] > 1 and x.stride(-1) != 1):
         raise ValueError(f"{name} must lie on {like.device}, its elements next to each other")
     return x.data_ptr()
 

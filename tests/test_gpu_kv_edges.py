@@ -227,3 +227,18 @@ def test_numbers_that_do_not_fit_the_interface_are_refused(native, monkeypatch):
         with pytest.raises((ValueError, M.MackoError)):
             cache.attend(q, tables, lengths, **more)
     assert (cache.attend(q, tables, lengths, window=2 ** 31 - 1, most_queries=2 ** 31 - 1, longest=2 ** 31 - 1) == 0).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_tables_of_one_page_that_lie_next_to_each_other(native, monkeypatch):
+    """A table of one entry has no next one: its stride says nothing."""
+    if not native:
+        monkeypatch.setattr(M.binding, "_native", None)
+    cache = pool(rng(1), 4, 16, 1, 64)
+    tables, lengths = np.array([[2], [0], [3]]), [5, 16, 9]
+    fill(rng(9), cache, tables, lengths)
+    q = normal(rng(3), 3, 2, 64).cuda()
+    want = cache.attend(q, ints(tables), ints(lengths))
+    assert torch.equal(cache.attend(q, ints([2, 0, 3])[None].t(), ints(lengths)), want)
+    with pytest.raises((ValueError, M.MackoError)):
+        cache.attend(q, ints([[2, 0, 3], [0, 0, 0]]).t(), ints(lengths))
