@@ -550,11 +550,15 @@ MACKO_API int macko_last_hip_error(void);
  *                       tests of the give-up path; the chain then reports MACKO_E_WAIT_EXPIRED)
  *   "spmm_kernel"       how macko_spmm takes a batch that both ways serve: 0 by estimates of both times,
  *                       1 pieces of vectors on the vector units, 2 the matrix cores
+ *   "attention_kernel"  how macko_kv_attention takes a call: 0 by estimates of both times, 1 the kernel for few rows,
+ *                       2 the one for many
+ *   "attention_parts"   parts that it deals a sequence's tokens out to, at most (1 .. 256), 0 by estimate; the same
+ *                       for macko_kv_attention_workspace and the call (calls of 2^24 rows and more have one part)
  *   "gemv_block", "gemv_rows_per_wg", "gemv_ring" (2, 4 or 8), "gemv_resident",
  *   "gemv_wgs_per_cu"   the same for the dense GEMV
  * Settings are process wide and not thread safe: macko_set_tuning must not run
  * at the same time as any call that launches a kernel (macko_spmv, macko_spmv_group,
- * macko_spmv_many, macko_spmv_chain*, macko_spmm, macko_dense_gemv*) on another host
+ * macko_spmv_many, macko_spmv_chain*, macko_spmm, macko_dense_gemv*, macko_kv_attention*) on another host
  * thread; those calls read the settings without locking.  With all knobs at 0, which
  * is the state of a process that never calls macko_set_tuning, the launching calls
  * may run concurrently on any number of host threads (macko_spmv_many and

@@ -526,6 +526,8 @@ bool is_prompt(const Grid& g) { return g.rows >= 64; }
 
 constexpr int64_t kMostGrid = 65535;       // of a launch's second and third dimension
 
+bool may_join(const KvAttention& a) { return a.tokens * a.heads < int64_t{1} << 24; }      // a join has a workgroup a row, and a launch fewer than 2^32 threads
+
 struct Dealt {
   int64_t splits;
   double time;
@@ -553,7 +555,7 @@ Dealt deal(const KvAttention& a, bool prompt, int64_t row_blocks, int64_t units,
     return turns * (5.0 + steps * std::max(alone, busy * share)) + join;
   };
   Dealt best{1, time(1)};
-  if (a.tokens * a.heads >= int64_t{1} << 24) return best;      // a join has a workgroup a row, and a launch fewer than 2^32 threads
+  if (!may_join(a)) return best;
   for (const int splits : kTry) {
     if (splits > units) break;
     const double t = time(splits);
@@ -570,12 +572,14 @@ Grid grid_of(const KvAttention& a) {
   const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
   auto blocks_of = [&](bool prompt) { return (most_rows + rows_of_block(a, prompt) - 1) / rows_of_block(a, prompt); };
   auto dealt = [&](bool prompt) { return deal(a, prompt, std::max<int64_t>(1, blocks_of(prompt)), (longest + unit - 1) / unit, kv_piece_bytes(unit, a.pool.dim)); };
-  Dealt dealt_out = dealt(false);
-  bool prompt = false;
-  if (most_rows > kPromptRows) {
+  const Tuning& knobs = tuning();
+  bool prompt = knobs.attention_kernel == 2;
+  Dealt dealt_out = dealt(prompt);
+  if (knobs.attention_kernel == 0 && most_rows > kPromptRows) {
     const Dealt as_prompt = dealt(true);
     if (as_prompt.time < dealt_out.time) dealt_out = as_prompt, prompt = true;
   }
+  if (knobs.attention_parts > 0 && may_join(a)) dealt_out.splits = std::min({knobs.attention_parts, (longest + unit - 1) / unit, (int64_t)kMostSplits});
   const int64_t splits = dealt_out.splits, row_blocks = blocks_of(prompt), others = (int64_t)a.batch * a.pool.heads * row_blocks;
   g.rows = rows_of_block(a, prompt);
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
