@@ -140,3 +140,37 @@ def test_many_sequences(batch, kv_heads, shared, asked, kernel, dtype):
     want = ref.attend(ref.to_numpy(q), cache.data.cpu().numpy(), page, tables, lengths, start)
     got, sums = cache.attend(q.cuda(), ints(tables), ints(lengths), start=ints(start), most_queries=asked, sums=True)
     check_attention(got, sums, *want, dtype)
+
+
+@pytest.mark.parametrize("parts", [1, 3])
+@pytest.mark.parametrize("page,window", [(16, 0), (256, 0), (64, 2990)])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_blocks_that_are_done_again(dim, page, window, parts):
+    """bf16 results of rows for which one token without a value is 60 powers of two ahead, beside rows that see all tokens alike; one group of values is not a
+    number, and the tokens that the last rows do not see are."""
+    named(MANY, parts)
+    g = rng(dim + page)
+    tokens, asked, gap = 3000, 150, 60.0
+    cache = pool(g, -(-tokens // page), page, 1, dim)
+    tables = sequences(g, cache, [tokens])
+    slots = tables[0, np.arange(tokens) // page] * page + np.arange(tokens) % page
+    k, v = normal(g, tokens, 1, dim), normal(g, tokens, 1, dim) + 1
+    k[..., :32] = 0
+    first = 100                                                  # with the window: the last rows see from 10 on
+    k[first, 0, :32], v[first] = 1, 0
+    v[1, 0, 5] = float("nan")                                    # a group that the window hides from all rows but the first ones
+    cache.append(None, k.cuda(), v.cuda(), None, ints(slots))
+    q = torch.zeros((asked, 1, dim), dtype=torch.bfloat16)
+    q[::2, :, :32] = 1.0
+    scale = gap * np.log(2) / 32
+    got = ref.to_numpy(cache.attend(q.cuda(), ints(tables), ints([tokens]), start=ints([0, asked]), most_queries=asked, scale=scale, window=window))
+    values = ref.read(cache.data.cpu().numpy(), page, dim, slots)[1][:, 0]
+    for i in range(asked):
+        p = tokens - asked + i
+        lo = max(0, p - window + 1) if window else 0
+        w = np.exp(-32 * float(np.float32(scale))) if i % 2 == 0 else 1.0
+        weight = np.where(np.arange(lo, p + 1) == first, 1.0, w)
+        want = weight @ values[lo:p + 1] / weight.sum()
+        fine = ~np.isnan(want)
+        assert np.array_equal(np.isnan(got[i, 0]), ~fine) and fine.sum() == dim - 32 * (lo <= 1)
+        assert np.linalg.norm((got[i, 0] - want)[fine]) <= (base.HALF[torch.bfloat16] + 2.0 ** -14) * np.linalg.norm(want[fine])
