@@ -386,7 +386,8 @@ MACKO_API int macko_dense_gemv_group(int n, const void* const* W_dev, const int6
  * 16-bit tensors are fp16 or bf16 (`type`), the same for all of a call; element
  * d of head h of token t lies at [t * ..._token + h * ..._head + d], strides in
  * elements (>= 0 for inputs; of outputs no two elements may share a place).
- * Sums, norms and the softmax are held in 32 bits; results are rounded once.
+ * Sums, norms and the softmax are held in 32 bits; results are rounded once (what
+ * macko_kv_attention's products take of scores and weights is said there).
  * Row counts, positions, slots, lengths and tables are int32 on the device.
  * These calls only enqueue on `stream`. */
 typedef enum macko_type { MACKO_FP16 = 0, MACKO_BF16 = 1 } macko_type;
@@ -477,6 +478,9 @@ MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const
  * tokens t <= p, with a window > 0 only those with t > p - window.  Head h reads
  * key/value head h / (heads / kv_heads).
  *   out = sum over seen t of softmax(scale * q.k_t) v_t,   sums = log sum exp(scale * q.k_t)
+ * Scores come from the matrix cores' 8-bit products, of queries in parts with the keys as they are held.  A channel of a query is exact to 2^-22 of the
+ * largest of its group of 32 or better, and the products are lined up with the largest before they are added: of all their magnitudes together a score is
+ * off by 2^-20 in the mean and 2^-15 at most where they are of like size, and by 2^-14 and 2^-11 where some are thousands of times the others.
  * The sum is divided last: where it passes 2^128 on the way (weights go up to 2^8 there), results are infinite.
  * A query that sees nothing gets zeros and a sum of -infinity.  A weight goes into its products with 16 bits, whatever its size; calls of many queries in
  * bf16 without sums_dev may take 11 bits, where no row's results are off by more than half a unit in the last place of its largest for that.  What lies in

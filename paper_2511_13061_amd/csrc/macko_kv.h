@@ -52,11 +52,6 @@ __device__ inline float to_float(uint32_t bits16) {
   return (float)__builtin_bit_cast(_Float16, (uint16_t)bits16);
 }
 template <bool BF>
-__device__ inline uint32_t to_bits(float x) {          // round to nearest even
-  if (BF) return __builtin_bit_cast(uint16_t, (__bf16)x);
-  return __builtin_bit_cast(uint16_t, (_Float16)x);
-}
-template <bool BF>
 __device__ inline void unpack8(Packed8 p, float* x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -65,7 +60,7 @@ __device__ inline void unpack8(Packed8 p, float* x) {
   }
 }
 template <bool BF>
-__device__ inline uint32_t pack2(float x, float y) {
+__device__ inline uint32_t pack2(float x, float y) {   // round to nearest even
   if (BF) {
     typedef __bf16 B2 __attribute__((ext_vector_type(2)));
     const B2 p = {(__bf16)x, (__bf16)y};

@@ -5,7 +5,10 @@
 //   scores   S^T = K Q^T by mfma_scale 16x16x128: keys go to the matrix cores as they lie in memory, 4-bit codes and the group's byte as the
 //            block scale, without an instruction of the vector units.  Queries are 8-bit parts, each what the ones before left over (fp16: 3,
 //            bf16: 2), with a scale of their own per 32 channels: together they hold every bit of a query down to 2^-18 (2^-13) of its group's largest.
-//   softmax  running maximum and sum in 32 bits.  Column r of S^T is row r, so a lane holds 8 scores of one row; the running maximum moves
+//            The instruction lines its products up with the largest before it adds them.  Measured, of the sum of their magnitudes: normally distributed
+//            queries and keys 2^-20 off in the mean, 2^-15.4 at worst; one product of 4000 beside 31 to 255 of about 1 2^-14.5 and 2^-12; heavy tails
+//            (times e^(2x), x normal) 2^-15 and 2^-11.2.
+//   softmax  running maximum and sum in 32 bits, the sum anew every 32 steps.  Column r of S^T is row r, so a lane holds 8 scores of one row; the running maximum moves
 //            only when a score is more than 2^8 above it, and only then do lanes talk to each other.
 //   values   O^T += V^T P^T by mfma 16x16x32 bf16: codes are exact in bf16 with any scale; weights go in as two bf16 parts (16 bits).
 //            The lanes of S^T that hold a token's weights are those that P^T needs: nothing moves between lanes.

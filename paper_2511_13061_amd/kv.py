@@ -1,6 +1,7 @@
 """Heads between a decoder layer's products: rotation, the paged 4-bit key/value cache, attention over it.
 
-Same names as the C ABI (``include/macko.h``, "keys and values in 4 bits"), argument checks and marshalling only.
+Same names as the C ABI (``include/macko.h``, "keys and values in 4 bits"), argument checks and marshalling only.  For inference: results have no
+gradient, also where an argument requires one.
 """
 from __future__ import annotations
 
