@@ -251,10 +251,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention_k
           for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
         }
         const float base = top[rt] == -INFINITY ? 0.f : -top[rt] * unit;       // nothing seen yet: weights of 2^-inf, not NaN
-        float weight[8];
+        float weight[8], more = 0.f;                       // `more`: of the step alone, for the same reason as lds_whole
 #pragma unroll
-        for (int i = 0; i < 8; ++i) weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
-        sum[rt] += ((weight[0] + weight[1]) + (weight[2] + weight[3])) + ((weight[4] + weight[5]) + (weight[6] + weight[7]));
+        for (int i = 0; i < 8; ++i) {
+          weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, base));
+          more = i == 0 ? weight[0] : more + weight[i];
+        }
+        sum[rt] += more;
         parts_of<false>(weight, p_hi[rt], p_lo[rt]);
       }
       if (careful || at + kTile > seq.length) {

@@ -26,7 +26,7 @@ def by_estimate_again():
 
 
 # parts up to 16 are joined by one kernel, more of them by another
-WAYS = [(FEW, 1), (FEW, 3), (FEW, 40), (MANY, 1), (MANY, 3), (MANY, 40)]
+WAYS = [(FEW, 1), (FEW, 40), (MANY, 1), (MANY, 3)]
 way = pytest.mark.parametrize("way", WAYS, ids=lambda w: f"{'few' if w[0] == FEW else 'many'}-{w[1]}")
 
 
