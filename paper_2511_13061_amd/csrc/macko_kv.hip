@@ -108,7 +108,9 @@ __device__ inline uint32_t turn_bytes(uint32_t word, int lane) {
 }
 
 // Memory bounds it: 8191 tokens of 40 heads with 128 channels, normalised and turned, 33 us (5.1 TB/s; a copy reaches 4.8 to 5.2); 16384 tokens of 32 heads into
-// the cache, q, k and v, 74 us.  One token takes 3 us, a launch's own time.
+// the cache, q, k and v, 74 us.  One token takes 3 us, a launch's own time.  By width (1024 channels of keys a token, 4 times as many of queries; TB/s): 32 channels
+// 3.7, 64 4.7, 96 4.1, 128 4.9, 160 3.7, 192 3.9, 224 4.1, 256 4.8: value codes go in whole words with 128 channels and byte by byte otherwise, and with
+// other than powers of two some lanes have no channels (4 of 16 with 96, 4 to 12 of 32 with 160 to 224).
 // Queries, keys and values have workgroups of their own.  A group of lanes takes BUNDLE heads of a token, whose loads are under way together;
 // position, table row and weight serve all of them.
 template <bool BF, int BUNDLE>
@@ -270,6 +272,7 @@ __device__ inline Packed8 decode8(uint32_t word, uint32_t byte) {
 }
 
 // Memory bounds it, and it writes four fifths of what it moves: 65536 slots of 8 heads with 128 channels 52 us, 6.4 TB/s (writing alone reaches 6.9).
+// By width, TB/s: 32 channels 3.8, 64 5.8, 96 5.1, 160 5.4, 192 5.7, 224 5.8, 256 6.4.
 template <bool BF, int BUNDLE>
 __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
   const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1), groups = kBlock >> a.lane_bits, n = a.pool.dim / 32;

@@ -10,9 +10,9 @@
 //   sums     of the weights come from the matrix cores too (a row of ones), 512 tokens at a time; those are added up with what rounding leaves out.
 // 64 tokens, because their keys and a step's scores are what the registers hold of two tiles of rows for two wavefronts on a SIMD; that is what hides one
 // wavefront's softmax behind another's products, as far as it is hidden.  1024 queries on each of 2 sequences of 8192 tokens, 32 heads on 8 of 128 channels, bf16:
-// 303 us, 850 TFLOP/s of the 1340 to 1373 that a product of 8192 x 8192 matrices reaches.  Of the 5700 cycles of a step on a SIMD the matrix cores are busy for
-// some 2200 (a score takes two parts of its query, at twice the rate of 16 bits) and the vector units for some 2600, so
-// that what is left is their overlap.  Tried for that, without gain: priorities of wavefronts around either half (1.5 % here, 9 % slower with 256 channels), all
+// 303 us, 850 TFLOP/s of the 1340 to 1385 that a product of 8192 x 8192 matrices reaches.  Of the 6200 cycles in which a SIMD does a step of each of its
+// wavefronts the matrix core is busy for 2180 (a score takes two parts of its query, at twice the rate of 16 bits) and the vector unit for 2640
+// (profiles/kv_prompt_kernel_counters.txt), so that what is left is their overlap.  Tried for that, without gain: priorities of wavefronts around either half (1.5 % here, 9 % slower with 256 channels), all
 // of a step's scores before its first weight (256 registers), loads a step earlier, eight wavefronts to a workgroup, three workgroups for narrow heads.
 #include "macko_kv_attention.h"
 
