@@ -483,7 +483,8 @@ MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const
  * off by 2^-20 in the mean and 2^-15 at most where they are of like size, and by 2^-14 and 2^-11 where some are thousands of times the others.
  * The sum is divided last: where it passes 2^128 on the way (weights go up to 2^8 there), results are infinite.
  * A query that sees nothing gets zeros and a sum of -infinity.  A weight goes into its products with 16 bits, whatever its size; calls of many queries in
- * bf16 without sums_dev may take 11 bits, where no row's results are off by more than half a unit in the last place of its largest for that.  What lies in
+ * bf16 without sums_dev may round it to 11 (and weights below 2^-24 of a row's largest to fewer, where all of that comes to less than half a unit in the
+ * last place of the row's largest result).  What lies in
  * tokens that a query does not see, in the rest of pages and in table entries that no
  * query of the sequence needs has no effect on it, NaN included (values that other
  * queries see may decide how a query's own are multiplied, and change its last place).  A table entry that a
