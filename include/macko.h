@@ -520,6 +520,77 @@ MACKO_API int64_t macko_kv_attention_workspace(const macko_kv_cache_t* cache, co
 MACKO_API int macko_kv_attention(const macko_kv_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
                                  int64_t workspace_bytes, void* stream);
 
+/* ---- keys and values in 8 bits ---------------------------------------------- */
+
+/* The same cache with 8.02 bits a value at most, for models that lose too much with 4: blocks of 16 tokens of
+ * one key/value head, whose keys share a byte b and whose values share another, a factor 2^(b-127); each value has
+ * an 8-bit code of the format E4M3 (as in "8-bit values": 448 at most, no infinities).  b is the least one from
+ * 1 to 246 that brings the block's largest finite magnitude to 448 times the factor at most; codes are rounded to nearest, ties to
+ * even, and stop at 448.  What is not finite is stored, and reads, as NaN, and has no part in b.
+ * A block fills token by token: where new tokens join others, b becomes the larger one of what the block has and
+ * what the new ones need, and if it grows, the codes of the tokens in front of them are rounded again to the new factor
+ * (which changes those alone that fall below 2^-6 of it).  A token at the first place of a block begins it anew, whatever lay
+ * there; what lies behind the new tokens keeps its codes.
+ *
+ * Types, strides, streams and the rest of the conventions are those of the 4-bit cache. */
+
+/* A pool of pages.  codes_dev and scales_dev: macko_kv8_cache_bytes of device memory, 16- and 2-byte aligned, caller
+ * owned, of any content.  page_size and head_dim (D) as for macko_kv_cache.  For each page, key/value head and block of 16 tokens
+ * of the page, in this order, codes_dev holds
+ *   key codes    [16][D]
+ *   value codes  [4][D][4]    byte [t/4][channel][t%4]
+ * and scales_dev the byte of the keys and the byte of the values. */
+typedef struct macko_kv8_cache {
+  void* codes_dev;
+  void* scales_dev;
+  int64_t pages;
+  int32_t page_size, kv_heads, head_dim;
+} macko_kv8_cache_t;
+
+/* Bytes of such a pool's codes, and in *scale_bytes (may be NULL) of its scales, or a negative macko_status. */
+MACKO_API int64_t macko_kv8_cache_bytes(const macko_kv8_cache_t* cache, int64_t* scale_bytes);
+
+/* New tokens: q and k are normalised and turned, q goes to q_out, k and v go to the cache.  The tokens are the last
+ * ones of `batch` sequences, as in macko_kv_attention: sequence b has lengths_dev[b] tokens with them (below 0 counts
+ * as 0), token t in page tables_dev[b * table_stride + t / page_size]; its new ones are the rows start_dev[b] ..
+ * start_dev[b+1] - 1 (start_dev NULL: row b, tokens == batch), in order.  All rows of q are turned, of a sequence or not.
+ * Rows before a sequence's first token (more rows than tokens), rows that are no sequence's, and tokens whose table entry names no page or
+ * is missing are stored nowhere.  A position outside the table makes the token's q_out and its stored keys NaN.
+ * No page that a call writes to may be another sequence's that it writes to (whole pages in front may be shared).  heads = 0: no
+ * queries.  One launch. */
+typedef struct macko_kv8_append_args {
+  int64_t tokens;
+  int32_t heads, type, batch;
+  const void* q_dev;
+  int64_t q_token, q_head;
+  void* q_out_dev;              /* may be q_dev with the same strides */
+  int64_t q_out_token, q_out_head;
+  const void* k_dev;
+  int64_t k_token, k_head;
+  const void* v_dev;
+  int64_t v_token, v_head;
+  const int32_t* tables_dev;    /* [batch][table_width] */
+  int64_t table_stride;
+  int32_t table_width;
+  const int32_t* lengths_dev;   /* [batch] */
+  const int32_t* start_dev;     /* [batch + 1], from 0 to tokens, or NULL */
+  const void* q_weight_dev;
+  const void* k_weight_dev;
+  macko_rotation_t rotation;
+} macko_kv8_append_args_t;
+MACKO_API int macko_kv8_append(const macko_kv8_cache_t* cache, const macko_kv8_append_args_t* args, void* stream);
+
+/* macko_kv_read of this cache.  A slot below 0 or outside the pool reads as zeros; what fp16 does not reach reads as an infinity. */
+MACKO_API int macko_kv8_read(const macko_kv8_cache_t* cache, int64_t tokens, const int32_t* slots_dev, int type,
+                             void* k_out_dev, int64_t k_token, int64_t k_head, void* v_out_dev, int64_t v_token,
+                             int64_t v_head, void* stream);
+
+/* macko_kv_attention over this cache: the same arguments, limits and promises, but for
+ * these.  Keys and values are exact; scores are sums in 32 bits of exact products of the queries as they are with the keys. */
+MACKO_API int64_t macko_kv8_attention_workspace(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args);
+MACKO_API int macko_kv8_attention(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
+                                  int64_t workspace_bytes, void* stream);
+
 /* ---- housekeeping ---------------------------------------------------------- */
 
 /* Waits until the device is idle if the handle owns device memory (that of the GPU encoder). */

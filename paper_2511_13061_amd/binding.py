@@ -21,7 +21,8 @@ EXPORTED_SYMBOLS = [
     "macko_decode", "macko_encode_fp8", "macko_encode_device_fp8", "macko_wrap_device_fp8", "macko_host_values_fp8", "macko_decode_fp8", "macko_check_device", "macko_columns_device", "macko_decode_device", "macko_spmv", "macko_dense_gemv", "macko_spmv_group", "macko_spmv_many", "macko_spmv_chain", "macko_spmv_chain_static", "macko_chain_status", "macko_dense_gemv_group", "macko_spmm", "macko_destroy", "macko_trim", "macko_status_string",
     "macko_last_hip_error", "macko_set_tuning", "macko_get_tuning",
     "macko_kv_cache_bytes", "macko_rope_table", "macko_rotate", "macko_kv_append", "macko_kv_read",
-    "macko_kv_attention_workspace", "macko_kv_attention",
+    "macko_kv_attention_workspace", "macko_kv_attention", "macko_kv8_cache_bytes", "macko_kv8_append", "macko_kv8_read",
+    "macko_kv8_attention_workspace", "macko_kv8_attention",
 ]
 
 
@@ -159,7 +160,8 @@ def load_library():
     if native is not None:
         native.bind(*[ctypes.cast(f, vp).value for f in (
             lib.macko_spmv, lib.macko_spmm, lib.macko_decode_device, lib.macko_rotate, lib.macko_kv_append, lib.macko_kv_read,
-            lib.macko_kv_attention_workspace, lib.macko_kv_attention)])
+            lib.macko_kv_attention_workspace, lib.macko_kv_attention, lib.macko_kv8_append, lib.macko_kv8_read,
+            lib.macko_kv8_attention_workspace, lib.macko_kv8_attention)])
         _native = native
     _lib = lib
     return lib

@@ -34,6 +34,10 @@ decltype(&macko_kv_append) g_append = nullptr;
 decltype(&macko_kv_read) g_read = nullptr;
 decltype(&macko_kv_attention_workspace) g_workspace = nullptr;
 decltype(&macko_kv_attention) g_attention = nullptr;
+decltype(&macko_kv8_append) g_append8 = nullptr;
+decltype(&macko_kv8_read) g_read8 = nullptr;
+decltype(&macko_kv8_attention_workspace) g_workspace8 = nullptr;
+decltype(&macko_kv8_attention) g_attention8 = nullptr;
 
 // A forked child may not use its parent's device.  PyTorch's Python calls refuse that with an error, the C++ calls below do not:
 // in a child the functions serve nothing, and the general way says what there is to say.
@@ -199,8 +203,9 @@ PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // The cache's geometry and its device, from their address and number.
-const macko_kv_cache_t* cache_of(PyObject* address, PyObject* device, c10::DeviceIndex* current) {
-  const auto* c = static_cast<const macko_kv_cache_t*>(PyLong_AsVoidPtr(address));
+template <class Cache = macko_kv_cache_t>
+const Cache* cache_of(PyObject* address, PyObject* device, c10::DeviceIndex* current) {
+  const auto* c = static_cast<const Cache*>(PyLong_AsVoidPtr(address));
   const long d = PyLong_AsLong(device);
   *current = c10::hip::current_device();
   return d == *current ? c : nullptr;
@@ -266,16 +271,16 @@ PyObject* two(int status, const at::Tensor& a, PyObject* given_a, const at::Tens
   return pair;
 }
 
-// kv_read(cache, device, slots, bf16, k_out, v_out)
-PyObject* kv_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+template <class Cache, class Read>
+PyObject* read_of(PyObject* const* args, Py_ssize_t n, Read read) {
   HANDLE_TH_ERRORS
   if (n != 6) return PyErr_Format(PyExc_TypeError, "6 arguments");
   c10::DeviceIndex device;
-  const macko_kv_cache_t* cache = cache_of(args[0], args[1], &device);
+  const Cache* cache = cache_of<Cache>(args[0], args[1], &device);
   const Given slots(args[2]), k(args[4]), v(args[5]);
   const bool bf16 = PyObject_IsTrue(args[3]);
   if (PyErr_Occurred()) return nullptr;
-  if (!g_read || g_forked || !cache || !slots.t || slots.t->dim() != 1 || !k.fine || !v.fine) Py_RETURN_NONE;
+  if (!read || g_forked || !cache || !slots.t || slots.t->dim() != 1 || !k.fine || !v.fine) Py_RETURN_NONE;
   const at::ScalarType scalar = bf16 ? at::kBFloat16 : at::kHalf;
   const int64_t tokens = slots.t->size(0), heads = cache->kv_heads, dim = cache->head_dim;
   if (!ints_fit(*slots.t, tokens, device) || (k.t && !made_fits(*k.t, tokens, heads, dim, scalar, device)) || (v.t && !made_fits(*v.t, tokens, heads, dim, scalar, device)))
@@ -288,25 +293,28 @@ PyObject* kv_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (!k.t) made[0] = at::empty({tokens, heads, dim}, options);
     if (!v.t) made[1] = at::empty({tokens, heads, dim}, options);
     const at::Tensor &x = k.t ? *k.t : made[0], &y = v.t ? *v.t : made[1];
-    status = g_read(cache, tokens, static_cast<const int32_t*>(slots.t->data_ptr()), bf16 ? MACKO_BF16 : MACKO_FP16, x.data_ptr(), x.stride(0), x.stride(1), y.data_ptr(),
+    status = read(cache, tokens, static_cast<const int32_t*>(slots.t->data_ptr()), bf16 ? MACKO_BF16 : MACKO_FP16, x.data_ptr(), x.stride(0), x.stride(1), y.data_ptr(),
                     y.stride(0), y.stride(1), c10::hip::getCurrentHIPStream().stream());
   }
   return two(status, made[0], args[4], made[1], args[5]);
   END_HANDLE_TH_ERRORS
 }
+// kv_read(cache, device, slots, bf16, k_out, v_out)
+PyObject* kv_read(PyObject*, PyObject* const* args, Py_ssize_t n) { return read_of<macko_kv_cache_t>(args, n, g_read); }
+PyObject* kv8_read(PyObject*, PyObject* const* args, Py_ssize_t n) { return read_of<macko_kv8_cache_t>(args, n, g_read8); }
 
-// kv_attend(cache, device, q, tables, lengths, start, most_queries, longest or None, scale or None, window, sums, out)
-PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
+template <class Cache, class Workspace, class Attention>
+PyObject* attend_of(PyObject* const* args, Py_ssize_t n, Workspace workspace, Attention attention) {
   HANDLE_TH_ERRORS
   if (n != 12) return PyErr_Format(PyExc_TypeError, "12 arguments");
   c10::DeviceIndex device;
-  const macko_kv_cache_t* cache = cache_of(args[0], args[1], &device);
+  const Cache* cache = cache_of<Cache>(args[0], args[1], &device);
   const Given q(args[2]), tables(args[3]), lengths(args[4]), start(args[5]), out(args[11]);
   const int64_t most = PyLong_AsLongLong(args[6]), window = PyLong_AsLongLong(args[9]), longest = args[7] == Py_None ? -1 : PyLong_AsLongLong(args[7]);
   const double scale = args[8] == Py_None ? 0.0 : PyFloat_AsDouble(args[8]);
   const bool sums = PyObject_IsTrue(args[10]);
   if (PyErr_Occurred()) return nullptr;
-  if (!g_attention || g_forked || !cache || !q.t || !tables.t || !lengths.t || !start.fine || !out.fine || q.t->dim() != 3 || tables.t->dim() != 2 || lengths.t->dim() != 1)
+  if (!attention || g_forked || !cache || !q.t || !tables.t || !lengths.t || !start.fine || !out.fine || q.t->dim() != 3 || tables.t->dim() != 2 || lengths.t->dim() != 1)
     Py_RETURN_NONE;
   const int64_t tokens = q.t->size(0), heads = q.t->size(1), dim = cache->head_dim, batch = lengths.t->size(0), width = tables.t->size(1);
   const at::ScalarType scalar = q.t->scalar_type();
@@ -329,7 +337,7 @@ PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
   int64_t status;
   {
     pybind11::gil_scoped_release unlocked;
-    status = g_workspace(cache, &a);
+    status = workspace(cache, &a);
     if (status >= 0) {
       at::Tensor work;
       if (!out.t) made = made_heads(tokens, heads, dim, *q.t);
@@ -340,20 +348,73 @@ PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
         a.sums_dev = static_cast<float*>(total.data_ptr());
       }
       if (status > 0) work = at::empty({status}, q.t->options().dtype(at::kByte));
-      status = g_attention(cache, &a, status > 0 ? work.data_ptr() : nullptr, status, c10::hip::getCurrentHIPStream().stream());
+      status = attention(cache, &a, status > 0 ? work.data_ptr() : nullptr, status, c10::hip::getCurrentHIPStream().stream());
     }
   }
   if (sums) return two((int)status, made, args[11], total, Py_None);
   return result((int)status, made, args[11]);
   END_HANDLE_TH_ERRORS
 }
+// kv_attend(cache, device, q, tables, lengths, start, most_queries, longest or None, scale or None, window, sums, out)
+PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n) { return attend_of<macko_kv_cache_t>(args, n, g_workspace, g_attention); }
+PyObject* kv8_attend(PyObject*, PyObject* const* args, Py_ssize_t n) { return attend_of<macko_kv8_cache_t>(args, n, g_workspace8, g_attention8); }
+
+// kv8_append(cache, device, q, k, v, positions, tables, lengths, start, table, q_weight, k_weight, eps, interleaved, q_out): True without queries
+PyObject* kv8_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 15) return PyErr_Format(PyExc_TypeError, "15 arguments");
+  c10::DeviceIndex device;
+  const macko_kv8_cache_t* cache = cache_of<macko_kv8_cache_t>(args[0], args[1], &device);
+  const Given q(args[2]), k(args[3]), v(args[4]), positions(args[5]), tables(args[6]), lengths(args[7]), start(args[8]), table(args[9]), q_weight(args[10]), k_weight(args[11]),
+      out(args[14]);
+  const double eps = PyFloat_AsDouble(args[12]);
+  const int interleaved = PyObject_IsTrue(args[13]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!g_append8 || g_forked || !cache || !k.t || !v.t || !tables.t || !lengths.t || !start.fine || k.t->dim() != 3 || tables.t->dim() != 2 || lengths.t->dim() != 1 || !q.fine || !out.fine ||
+      (q.t && q.t->dim() != 3))
+    Py_RETURN_NONE;
+  const at::ScalarType scalar = k.t->scalar_type();
+  const int64_t tokens = k.t->size(0), heads = q.t ? q.t->size(1) : 0, dim = cache->head_dim, batch = lengths.t->size(0), width = tables.t->size(1);
+  macko_kv8_append_args_t a{};
+  a.type = type_of(*k.t);
+  if (a.type < 0 || tokens == 0 || heads > INT32_MAX || batch > INT32_MAX || width > INT32_MAX || !heads_fit(*k.t, tokens, cache->kv_heads, dim, scalar, device) ||
+      !heads_fit(*v.t, tokens, cache->kv_heads, dim, scalar, device) || !ints_fit(*lengths.t, batch, device) || tables.t->size(0) != batch || tables.t->scalar_type() != at::kInt ||
+      (width > 1 && tables.t->stride(1) != 1) || !on(*tables.t, device) || (start.t ? !ints_fit(*start.t, batch + 1, device) : batch != tokens) ||
+      (q.t && !heads_fit(*q.t, tokens, heads, dim, scalar, device)) || !weight_fits(k_weight, dim, scalar, device) || !weight_fits(q_weight, dim, scalar, device) ||
+      !rotation_of(positions, table, tokens, interleaved, eps, device, &a.rotation) || (q.t && out.t && !made_fits(*out.t, tokens, heads, dim, scalar, device)))
+    Py_RETURN_NONE;
+  a.tokens = tokens, a.heads = (int32_t)heads, a.batch = (int32_t)batch;
+  a.k_dev = k.t->data_ptr(), a.k_token = k.t->stride(0), a.k_head = k.t->stride(1);
+  a.v_dev = v.t->data_ptr(), a.v_token = v.t->stride(0), a.v_head = v.t->stride(1);
+  a.tables_dev = static_cast<const int32_t*>(tables.t->data_ptr()), a.table_stride = tables.t->stride(0), a.table_width = (int32_t)width;
+  a.lengths_dev = static_cast<const int32_t*>(lengths.t->data_ptr());
+  a.start_dev = start.t ? static_cast<const int32_t*>(start.t->data_ptr()) : nullptr;
+  a.k_weight_dev = k_weight.t ? k_weight.t->data_ptr() : nullptr;
+  a.q_weight_dev = q.t && q_weight.t ? q_weight.t->data_ptr() : nullptr;
+  at::Tensor made;
+  int status;
+  {
+    pybind11::gil_scoped_release unlocked;
+    if (q.t) {
+      if (!out.t) made = made_heads(tokens, heads, dim, *q.t);
+      const at::Tensor& y = out.t ? *out.t : made;
+      a.q_dev = q.t->data_ptr(), a.q_token = q.t->stride(0), a.q_head = q.t->stride(1);
+      a.q_out_dev = y.data_ptr(), a.q_out_token = y.stride(0), a.q_out_head = y.stride(1);
+    }
+    status = g_append8(cache, &a, c10::hip::getCurrentHIPStream().stream());
+  }
+  if (status == MACKO_OK && !q.t) Py_RETURN_TRUE;
+  return result(status, made, args[14]);
+  END_HANDLE_TH_ERRORS
+}
 
 // bind(addresses of macko_spmv, macko_spmm, macko_decode_device, macko_rotate, macko_kv_append, macko_kv_read, macko_kv_attention_workspace,
-// macko_kv_attention)
+// macko_kv_attention, macko_kv8_append, macko_kv8_read, macko_kv8_attention_workspace, macko_kv8_attention)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 8) return PyErr_Format(PyExc_TypeError, "8 arguments");
-  void* p[8];
-  for (int i = 0; i < 8; ++i) p[i] = PyLong_AsVoidPtr(args[i]);
+  constexpr int kCalls = 12;
+  if (n != kCalls) return PyErr_Format(PyExc_TypeError, "%d arguments", kCalls);
+  void* p[kCalls];
+  for (int i = 0; i < kCalls; ++i) p[i] = PyLong_AsVoidPtr(args[i]);
   if (PyErr_Occurred()) return nullptr;
   if (!g_spmv && pthread_atfork(nullptr, nullptr, [] { g_forked = true; }) != 0) return PyErr_NoMemory();
   g_spmv = reinterpret_cast<decltype(g_spmv)>(p[0]);
@@ -364,11 +425,16 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   g_read = reinterpret_cast<decltype(g_read)>(p[5]);
   g_workspace = reinterpret_cast<decltype(g_workspace)>(p[6]);
   g_attention = reinterpret_cast<decltype(g_attention)>(p[7]);
+  g_append8 = reinterpret_cast<decltype(g_append8)>(p[8]);
+  g_read8 = reinterpret_cast<decltype(g_read8)>(p[9]);
+  g_workspace8 = reinterpret_cast<decltype(g_workspace8)>(p[10]);
+  g_attention8 = reinterpret_cast<decltype(g_attention8)>(p[11]);
   Py_RETURN_NONE;
 }
 
 #define MACKO_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {MACKO_FAST(spmv), MACKO_FAST(spmm), MACKO_FAST(decode_device), MACKO_FAST(rotate), MACKO_FAST(kv_append), MACKO_FAST(kv_read), MACKO_FAST(kv_attend), MACKO_FAST(bind), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {MACKO_FAST(spmv), MACKO_FAST(spmm), MACKO_FAST(decode_device), MACKO_FAST(rotate), MACKO_FAST(kv_append), MACKO_FAST(kv_read), MACKO_FAST(kv_attend),
+                         MACKO_FAST(kv8_append), MACKO_FAST(kv8_read), MACKO_FAST(kv8_attend), MACKO_FAST(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -92,6 +92,14 @@ struct KvAttention {
   int32_t type;
 };
 bool kv_attention_fits(const KvAttention& a);        // in a launch
+// The arguments of a call over a pool, checked; `pointers`: they are needed too.
+int kv_attention_of(const KvPool& pool, const macko_kv_attention_args_t* g, bool pointers, KvAttention* a);
+
+// Checks of arguments, in macko_kv.hip
+bool aligned_to(const void* p, uintptr_t bytes);
+int check_head_dim(int64_t dim);
+bool heads_fine(const void* p, int64_t token, int64_t head);       // 16-bit heads of a call: there, on 2 bytes, with strides that stay far from 64 bits
+int check_rotation(const macko_rotation_t& r, int dim, int64_t tokens);
 // floats of workspace that the launch needs
 int64_t kv_attention_workspace(const KvAttention& a);
 int launch_kv_attention(const KvAttention& a, float* workspace, hipStream_t stream);

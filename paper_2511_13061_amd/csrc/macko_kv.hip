@@ -344,14 +344,18 @@ __global__ __launch_bounds__(kBlock) void table_kernel(const TableArgs a) {
 
 // ---- arguments ---------------------------------------------------------------
 
+}  // namespace
+
 bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
-int check_dim(int64_t dim) { return dim < 1 ? MACKO_E_INVALID_ARG : dim % 32 != 0 || dim > 256 ? MACKO_E_UNSUPPORTED : MACKO_OK; }
+int check_head_dim(int64_t dim) { return dim < 1 ? MACKO_E_INVALID_ARG : dim % 32 != 0 || dim > 256 ? MACKO_E_UNSUPPORTED : MACKO_OK; }
+
+namespace {
 
 // A pool's geometry; `data`: its memory is needed too.
 int pool_of(const macko_kv_cache_t* c, bool data, KvPool* p) {
   if (!c || c->pages < 0 || c->page_size < 1 || c->kv_heads < 1) return MACKO_E_INVALID_ARG;
-  if (int st = check_dim(c->head_dim)) return st;
+  if (int st = check_head_dim(c->head_dim)) return st;
   if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0) return MACKO_E_UNSUPPORTED;
   if (c->kv_heads > 65536 || c->pages > INT32_MAX / c->page_size) return MACKO_E_UNSUPPORTED;
   if (data && c->pages > 0 && (!c->data_dev || !aligned_to(c->data_dev, 16))) return MACKO_E_INVALID_ARG;
@@ -361,8 +365,10 @@ int pool_of(const macko_kv_cache_t* c, bool data, KvPool* p) {
   return MACKO_OK;
 }
 
-// 16-bit heads of a call: there, on 2 bytes, with strides that stay far from 64 bits.
 constexpr int64_t kMostStride = int64_t{1} << 31;        // times at most 2^31 tokens
+
+}  // namespace
+
 bool heads_fine(const void* p, int64_t token, int64_t head) {
   return p && aligned_to(p, 2) && token >= 0 && head >= 0 && token <= kMostStride && head <= kMostStride;
 }
@@ -373,6 +379,8 @@ int check_rotation(const macko_rotation_t& r, int dim, int64_t tokens) {
   if (r.rot > 0 && tokens > 0 && (!r.positions_dev || !aligned_to(r.positions_dev, 4) || (r.table_rows > 0 && !r.table_dev) || !aligned_to(r.table_dev, 16))) return MACKO_E_INVALID_ARG;
   return MACKO_OK;
 }
+
+namespace {
 
 int lane_bits_of(int dim) {
   int bits = 2;
@@ -419,11 +427,10 @@ void set_rotation(TurnArgs& a, const macko_rotation_t& r) {
   a.eps = r.eps;
 }
 
-// `pointers`: they are needed too
-int attention_of(const macko_kv_cache_t* cache, const macko_kv_attention_args_t* g, bool pointers, KvAttention* a) {
+}  // namespace
+
+int kv_attention_of(const KvPool& pool, const macko_kv_attention_args_t* g, bool pointers, KvAttention* a) {
   if (!g) return MACKO_E_INVALID_ARG;
-  KvPool pool;
-  if (int st = pool_of(cache, pointers, &pool)) return st;
   if (g->tokens < 0 || g->heads < 1 || g->batch < 0 || g->most_queries < 1 || g->window < 0 || g->longest < 0 || g->table_width < 0 || g->table_stride < 0 ||
       (g->type != MACKO_FP16 && g->type != MACKO_BF16) || g->heads % pool.heads != 0 || !std::isfinite(g->scale))
     return MACKO_E_INVALID_ARG;
@@ -440,6 +447,15 @@ int attention_of(const macko_kv_cache_t* cache, const macko_kv_attention_args_t*
                    g->tables_dev, g->table_stride, g->lengths_dev, g->start_dev, g->table_width, g->batch, g->heads, g->heads / pool.heads, window, g->scale,
                    (int32_t)std::max<int64_t>(1, std::min<int64_t>(g->most_queries, g->tokens)), g->tokens, g->longest, g->type};
   return kv_attention_fits(*a) ? MACKO_OK : MACKO_E_UNSUPPORTED;
+}
+
+namespace {
+
+int attention_of(const macko_kv_cache_t* cache, const macko_kv_attention_args_t* g, bool pointers, KvAttention* a) {
+  if (!g) return MACKO_E_INVALID_ARG;
+  KvPool pool;
+  if (int st = pool_of(cache, pointers, &pool)) return st;
+  return kv_attention_of(pool, g, pointers, a);
 }
 
 }  // namespace
@@ -471,7 +487,7 @@ int macko_rope_table(int64_t first, int64_t count, int rot, double base, double 
 int macko_rotate(int64_t tokens, int heads, int head_dim, int type, const void* x_dev, int64_t x_token, int64_t x_head, const macko_rotation_t* rotation,
                  const void* weight_dev, void* out_dev, int64_t out_token, int64_t out_head, void* stream) {
   if (tokens < 0 || heads < 0 || !rotation || (type != MACKO_FP16 && type != MACKO_BF16)) return MACKO_E_INVALID_ARG;
-  if (int st = check_dim(head_dim)) return st;
+  if (int st = check_head_dim(head_dim)) return st;
   if (int st = check_rotation(*rotation, head_dim, heads ? tokens : 0)) return st;
   if (tokens == 0 || heads == 0) return MACKO_OK;
   if (tokens > INT32_MAX || heads > 65536) return MACKO_E_UNSUPPORTED;

@@ -207,5 +207,10 @@ __device__ inline void parts_of(const float* w, V4i& hi, V4i& lo) {
 // (macko_kv_prompt.hip) many rows
 int launch_prompt(const KvAttention& a, const Grid& g, hipStream_t stream);
 int prompt_row_tiles(int dim);       // of a wavefront there
+// (macko_kv_attention.hip) the parts of rows that were split
+int launch_join(const KvAttention& a, const Grid& g, hipStream_t stream);
+
+constexpr int64_t kMostGrid = 65535;       // of a launch's second and third dimension
+inline bool may_join(const KvAttention& a) { return a.tokens * a.heads < int64_t{1} << 24; }      // a join has a workgroup a row, and a launch fewer than 2^32 threads
 
 }  // namespace macko

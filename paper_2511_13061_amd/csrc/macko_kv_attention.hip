@@ -530,9 +530,6 @@ constexpr int kPromptRows = 64;
 int rows_of_block(const KvAttention& a, bool prompt) { return prompt ? 16 * kWaves * prompt_row_tiles(a.pool.dim) : 16 * row_tiles(a); }
 bool is_prompt(const Grid& g) { return g.rows >= 64; }
 
-constexpr int64_t kMostGrid = 65535;       // of a launch's second and third dimension
-
-bool may_join(const KvAttention& a) { return a.tokens * a.heads < int64_t{1} << 24; }      // a join has a workgroup a row, and a launch fewer than 2^32 threads
 
 struct Dealt {
   int64_t splits;
@@ -605,6 +602,15 @@ int launch_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
 }
 
 template <int NG, bool BF>
+int join_of(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  const int64_t rows = a.tokens * a.heads;
+  if (g.splits <= kFewSplits) hipLaunchKernelGGL((join_few_kernel<NG, BF>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, g);
+  else hipLaunchKernelGGL((join_kernel<NG, BF>), dim3((unsigned)rows), dim3(256), 0, stream, a, g);
+  MACKO_HIP_TRY(hipGetLastError());
+  return MACKO_OK;
+}
+
+template <int NG, bool BF>
 int launch_type(const KvAttention& a, const Grid& g, hipStream_t stream) {
   int status = MACKO_OK;
   bool one = true;
@@ -618,18 +624,16 @@ int launch_type(const KvAttention& a, const Grid& g, hipStream_t stream) {
     }
   }
   if (one) status = launch_of<NG, BF, 1>(a, g, stream);
-  if (status == MACKO_OK && g.splits > 1) {
-    const int64_t rows = a.tokens * a.heads;
-    if (g.splits <= kFewSplits) hipLaunchKernelGGL((join_few_kernel<NG, BF>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, g);
-    else hipLaunchKernelGGL((join_kernel<NG, BF>), dim3((unsigned)rows), dim3(256), 0, stream, a, g);
-    MACKO_HIP_TRY(hipGetLastError());
-  }
-  return status;
+  return status == MACKO_OK && g.splits > 1 ? join_of<NG, BF>(a, g, stream) : status;
 }
 
 template <int NG>
 int launch_dim(const KvAttention& a, const Grid& g, hipStream_t stream) {
   return a.type == MACKO_BF16 ? launch_type<NG, true>(a, g, stream) : launch_type<NG, false>(a, g, stream);
+}
+template <int NG>
+int join_dim(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  return a.type == MACKO_BF16 ? join_of<NG, true>(a, g, stream) : join_of<NG, false>(a, g, stream);
 }
 
 }  // namespace
@@ -638,6 +642,20 @@ bool kv_attention_fits(const KvAttention& a) {
   if (a.tokens == 0 || a.batch == 0) return true;
   const int64_t rows = a.tokens * a.heads;
   return rows <= kMostTokens && a.batch <= kMostGrid && a.shared <= 32768;
+}
+
+int launch_join(const KvAttention& a, const Grid& g, hipStream_t stream) {
+  switch (a.pool.dim / 32) {
+    case 1: return join_dim<1>(a, g, stream);
+    case 2: return join_dim<2>(a, g, stream);
+    case 3: return join_dim<3>(a, g, stream);
+    case 4: return join_dim<4>(a, g, stream);
+    case 5: return join_dim<5>(a, g, stream);
+    case 6: return join_dim<6>(a, g, stream);
+    case 7: return join_dim<7>(a, g, stream);
+    case 8: return join_dim<8>(a, g, stream);
+  }
+  return MACKO_E_UNSUPPORTED;
 }
 
 int64_t kv_attention_workspace(const KvAttention& a) {

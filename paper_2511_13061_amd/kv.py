@@ -30,6 +30,17 @@ class _CAppend(ctypes.Structure):
                 ("rotation", _CRotation)]
 
 
+class _CCache8(ctypes.Structure):
+    _fields_ = [("codes", _vp), ("scales", _vp), ("pages", _i64), ("page_size", _i32), ("kv_heads", _i32), ("head_dim", _i32)]
+
+
+class _CAppend8(ctypes.Structure):
+    _fields_ = [("tokens", _i64), ("heads", _i32), ("type", _i32), ("batch", _i32), ("q", _vp), ("q_token", _i64), ("q_head", _i64),
+                ("q_out", _vp), ("q_out_token", _i64), ("q_out_head", _i64), ("k", _vp), ("k_token", _i64), ("k_head", _i64),
+                ("v", _vp), ("v_token", _i64), ("v_head", _i64), ("tables", _vp), ("table_stride", _i64), ("table_width", _i32),
+                ("lengths", _vp), ("start", _vp), ("q_weight", _vp), ("k_weight", _vp), ("rotation", _CRotation)]
+
+
 class _CAttention(ctypes.Structure):
     _fields_ = [("tokens", _i64), ("heads", _i32), ("type", _i32), ("batch", _i32), ("q", _vp), ("q_token", _i64), ("q_head", _i64),
                 ("out", _vp), ("out_token", _i64), ("out_head", _i64), ("sums", _vp), ("tables", _vp), ("table_stride", _i64),
@@ -49,6 +60,14 @@ def _declare(lib) -> None:
     lib.macko_kv_attention_workspace.argtypes = [cp, ctypes.POINTER(_CAttention)]
     lib.macko_kv_attention_workspace.restype = _i64
     lib.macko_kv_attention.argtypes = [cp, ctypes.POINTER(_CAttention), _vp, _i64, _vp]
+    cp = ctypes.POINTER(_CCache8)
+    lib.macko_kv8_cache_bytes.argtypes = [cp, ctypes.POINTER(_i64)]
+    lib.macko_kv8_cache_bytes.restype = _i64
+    lib.macko_kv8_append.argtypes = [cp, ctypes.POINTER(_CAppend8), _vp]
+    lib.macko_kv8_read.argtypes = [cp, _i64, _vp, ctypes.c_int, _vp, _i64, _i64, _vp, _i64, _i64, _vp]
+    lib.macko_kv8_attention_workspace.argtypes = [cp, ctypes.POINTER(_CAttention)]
+    lib.macko_kv8_attention_workspace.restype = _i64
+    lib.macko_kv8_attention.argtypes = [cp, ctypes.POINTER(_CAttention), _vp, _i64, _vp]
 
 
 def _type_of(x) -> int:
@@ -173,6 +192,59 @@ def rotate(x, positions, table, weight=None, eps=1e-6, interleaved=False, out=No
     return out
 
 
+def _read(cache, name, slots, dtype, k_out, v_out, stream):
+    """The general way of a cache's read."""
+    torch = _need_torch()
+    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    with _on(cache.data.device, stream):
+        made = [torch.empty(shape, dtype=dtype, device=cache.data.device) if x is None else x for x in (k_out, v_out)]
+        if made[0].dtype != dtype:
+            raise ValueError("k_out and v_out must be of the type that is asked for")
+        kind = _type_of(made[0])
+        at = _ints(slots, "slots", (shape[0],), cache.data)
+        to = [_made_heads(x, what, shape, made[0]) for x, what in zip(made, ("k_out", "v_out"))]
+        cache._same(made[0])
+        _check(getattr(load_library(), name)(cache._p, shape[0], at, kind, *to[0], *to[1], _stream_ptr(stream)), name)
+    return made[0], made[1]
+
+
+def _attend(cache, name, q, tables, lengths, start, most_queries, longest, scale, window, sums, out, stream):
+    """The general way of a cache's attend."""
+    torch = _need_torch()
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens, heads, head_dim]")
+    kind, shape = _type_of(q), (q.shape[0], q.shape[1], cache.head_dim)
+    batch = lengths.shape[0] if lengths.dim() == 1 else -1
+    if tables.dim() != 2:
+        raise ValueError("tables must be [batch, pages]")
+    a = _CAttention(shape[0], shape[1], kind, batch)
+    a.q, a.q_token, a.q_head = _heads(q, "q", shape, cache._same(q))
+    a.lengths = _ints(lengths, "lengths", (batch,), q)
+    a.tables = _ints(tables, "tables", (batch, tables.shape[1]), q)
+    a.table_stride, a.table_width = tables.stride(0), tables.shape[1]
+    if start is not None:
+        a.start = _ints(start, "start", (batch + 1,), q)
+    elif batch != shape[0]:
+        raise ValueError("without start, q has one row a sequence")
+    a.most_queries, a.window = _whole(most_queries, "most_queries"), _whole(window, "window")
+    a.longest = a.table_width * cache.page_size if longest is None else _whole(longest, "longest", 64)
+    a.scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else scale
+    lib = load_library()
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        a.out, a.out_token, a.out_head = _made_heads(out, "out", shape, q)
+        total = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if sums else None
+        if sums:
+            a.sums = total.data_ptr()
+        size = getattr(lib, name + "_workspace")(cache._p, ctypes.byref(a))
+        if size < 0:
+            _check(int(size), name)
+        work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+        _check(getattr(lib, name)(cache._p, ctypes.byref(a), work.data_ptr() if size else None, size, _stream_ptr(stream)), name)
+    return (out, total) if sums else out
+
+
 class KvCache:
     """A pool of pages of keys and values in 4 bits (macko_kv_cache_t).
 
@@ -234,17 +306,7 @@ class KvCache:
             pair = binding._native.kv_read(self._address, self._device, slots, dtype == torch.bfloat16, k_out, v_out)
             if pair is not None:
                 return _made(pair, "macko_kv_read")
-        shape = (slots.shape[0], self.kv_heads, self.head_dim)
-        with _on(self.data.device, stream):
-            made = [torch.empty(shape, dtype=dtype, device=self.data.device) if x is None else x for x in (k_out, v_out)]
-            if made[0].dtype != dtype:
-                raise ValueError("k_out and v_out must be of the type that is asked for")
-            kind = _type_of(made[0])
-            at = _ints(slots, "slots", (shape[0],), self.data)
-            to = [_made_heads(x, name, shape, made[0]) for x, name in zip(made, ("k_out", "v_out"))]
-            self._same(made[0])
-            _check(load_library().macko_kv_read(self._p, shape[0], at, kind, *to[0], *to[1], _stream_ptr(stream)), "macko_kv_read")
-        return made[0], made[1]
+        return _read(self, "macko_kv_read", slots, dtype, k_out, v_out, stream)
 
     def attend(self, q, tables, lengths, start=None, most_queries=1, longest=None, scale=None, window=0, sums=False, out=None, stream=None):
         """macko_kv_attention of q [tokens, heads, head_dim] over the sequences' cached tokens.
@@ -257,39 +319,101 @@ class KvCache:
             y = binding._native.kv_attend(self._address, self._device, q, tables, lengths, start, most_queries, longest, scale, window, sums, out)
             if y is not None:
                 return _made(y, "macko_kv_attention")
+        return _attend(self, "macko_kv_attention", q, tables, lengths, start, most_queries, longest, scale, window, sums, out, stream)
+
+    def _same(self, x):
+        if x.device != self.data.device:
+            raise ValueError(f"tensors must lie on {self.data.device}, with the cache")
+        return x
+
+
+class KvCache8:
+    """A pool of pages of keys and values in 8 bits (macko_kv8_cache_t), a power of two for each block of 16 tokens and head.
+
+    data: uint8 [pages, kv_heads, page_size / 16, 2, 16 * head_dim], the codes of keys and values, and scales: uint8 [pages, kv_heads, page_size / 16, 2], both
+    on the GPU, allocated unless given (a loaded or shared pool: both)."""
+
+    def __init__(self, pages, page_size, kv_heads, head_dim, data=None, scales=None, device="cuda"):
         torch = _need_torch()
-        if q.dim() != 3:
-            raise ValueError("q must be [tokens, heads, head_dim]")
-        kind, shape = _type_of(q), (q.shape[0], q.shape[1], self.head_dim)
+        c = _CCache8(None, None, _whole(pages, "pages", 64), _whole(page_size, "page_size"), _whole(kv_heads, "kv_heads"), _whole(head_dim, "head_dim"))
+        size = load_library().macko_kv8_cache_bytes(ctypes.byref(c), None)
+        if size < 0:
+            _check(int(size), "macko_kv8_cache_bytes")
+        if (data is None) != (scales is None):
+            raise ValueError("data and scales are given together")
+        blocks = (c.pages, c.kv_heads, c.page_size // 16, 2)
+        made = []
+        for x, name, shape in ((data, "data", blocks + (16 * c.head_dim,)), (scales, "scales", blocks)):
+            if x is None:
+                x = torch.empty(shape, dtype=torch.uint8, device=device)
+            if x.dtype != torch.uint8:
+                raise TypeError(f"{name} must be uint8")
+            if tuple(x.shape) != shape or not x.is_contiguous() or not x.is_cuda:
+                raise ValueError(f"{name} must be a contiguous {list(shape)} tensor on the GPU")
+            made.append(x)
+        if made[0].device != made[1].device:
+            raise ValueError("data and scales must lie on one device")
+        c.codes, c.scales = made[0].data_ptr(), made[1].data_ptr()
+        self.data, self.scales, self._c, self._p = *made, c, ctypes.byref(c)
+        self._address, self._device = ctypes.addressof(c), self.data.device.index
+        self.pages, self.page_size, self.kv_heads, self.head_dim = c.pages, c.page_size, c.kv_heads, c.head_dim
+
+    def append(self, q, k, v, positions, tables, lengths, start=None, table=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, q_out=None, stream=None):
+        """macko_kv8_append: q and k [tokens, heads, head_dim] normalised (weights) and turned (table, positions), k and v into the cache as the last tokens
+        of the sequences that tables, lengths (with the new tokens) and start say, as in attend.  Returns q_out, which may be q; None without queries."""
+        if stream is None and binding._native is not None:
+            y = binding._native.kv8_append(self._address, self._device, q, k, v, positions, tables, lengths, start, table, q_weight, k_weight, eps, interleaved, q_out)
+            if y is not None:
+                return None if y is True else _made(y, "macko_kv8_append")
+        torch = _need_torch()
+        kind, tokens = _type_of(k), k.shape[0]
+        shape = (tokens, self.kv_heads, self.head_dim)
         batch = lengths.shape[0] if lengths.dim() == 1 else -1
         if tables.dim() != 2:
             raise ValueError("tables must be [batch, pages]")
-        a = _CAttention(shape[0], shape[1], kind, batch)
-        a.q, a.q_token, a.q_head = _heads(q, "q", shape, self._same(q))
-        a.lengths = _ints(lengths, "lengths", (batch,), q)
-        a.tables = _ints(tables, "tables", (batch, tables.shape[1]), q)
+        a = _CAppend8(tokens, 0, kind, batch)
+        a.k, a.k_token, a.k_head = _heads(k, "k", shape, self._same(k))
+        a.v, a.v_token, a.v_head = _heads(v, "v", shape, k)
+        a.lengths = _ints(lengths, "lengths", (batch,), k)
+        a.tables = _ints(tables, "tables", (batch, tables.shape[1]), k)
         a.table_stride, a.table_width = tables.stride(0), tables.shape[1]
         if start is not None:
-            a.start = _ints(start, "start", (batch + 1,), q)
-        elif batch != shape[0]:
-            raise ValueError("without start, q has one row a sequence")
-        a.most_queries, a.window = _whole(most_queries, "most_queries"), _whole(window, "window")
-        a.longest = a.table_width * self.page_size if longest is None else _whole(longest, "longest", 64)
-        a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
-        lib = load_library()
-        with _on(q.device, stream):
-            if out is None:
-                out = torch.empty(shape, dtype=q.dtype, device=q.device)
-            a.out, a.out_token, a.out_head = _made_heads(out, "out", shape, q)
-            total = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if sums else None
-            if sums:
-                a.sums = total.data_ptr()
-            size = lib.macko_kv_attention_workspace(self._p, ctypes.byref(a))
-            if size < 0:
-                _check(int(size), "macko_kv_attention")
-            work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
-            _check(lib.macko_kv_attention(self._p, ctypes.byref(a), work.data_ptr() if size else None, size, _stream_ptr(stream)), "macko_kv_attention")
-        return (out, total) if sums else out
+            a.start = _ints(start, "start", (batch + 1,), k)
+        elif batch != tokens:
+            raise ValueError("without start, there is one row a sequence")
+        a.k_weight = _weight(k_weight, "k_weight", k)
+        a.rotation = _rotation(k, positions, table, interleaved, eps)
+        with _on(k.device, stream):
+            if q is not None:
+                shape = (tokens, q.shape[1] if q.dim() == 3 else 0, self.head_dim)
+                a.heads = shape[1]
+                a.q, a.q_token, a.q_head = _heads(q, "q", shape, k)
+                a.q_weight = _weight(q_weight, "q_weight", q)
+                if q_out is None:
+                    q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
+                a.q_out, a.q_out_token, a.q_out_head = _made_heads(q_out, "q_out", shape, q)
+            _check(load_library().macko_kv8_append(self._p, ctypes.byref(a), _stream_ptr(stream)), "macko_kv8_append")
+        return q_out if q is not None else None
+
+    def read(self, slots, dtype=None, k_out=None, v_out=None, stream=None):
+        """macko_kv8_read: keys and values [tokens, kv_heads, head_dim] of the slots (int32, below 0: zeros), in dtype (float16 by default)."""
+        torch = binding._torch or _need_torch()
+        if dtype is None:
+            given = k_out if k_out is not None else v_out
+            dtype = torch.float16 if given is None else given.dtype
+        if stream is None and binding._native is not None and (dtype == torch.float16 or dtype == torch.bfloat16):
+            pair = binding._native.kv8_read(self._address, self._device, slots, dtype == torch.bfloat16, k_out, v_out)
+            if pair is not None:
+                return _made(pair, "macko_kv8_read")
+        return _read(self, "macko_kv8_read", slots, dtype, k_out, v_out, stream)
+
+    def attend(self, q, tables, lengths, start=None, most_queries=1, longest=None, scale=None, window=0, sums=False, out=None, stream=None):
+        """macko_kv8_attention: KvCache.attend over this cache."""
+        if stream is None and binding._native is not None:
+            y = binding._native.kv8_attend(self._address, self._device, q, tables, lengths, start, most_queries, longest, scale, window, sums, out)
+            if y is not None:
+                return _made(y, "macko_kv8_attention")
+        return _attend(self, "macko_kv8_attention", q, tables, lengths, start, most_queries, longest, scale, window, sums, out, stream)
 
     def _same(self, x):
         if x.device != self.data.device:
