@@ -591,6 +591,39 @@ MACKO_API int64_t macko_kv8_attention_workspace(const macko_kv8_cache_t* cache, 
 MACKO_API int macko_kv8_attention(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
                                   int64_t workspace_bytes, void* stream);
 
+/* ---- a prompt over its own keys and values ----------------------------------- */
+
+/* Causal attention of packed sequences over keys and values in 16 bits, before they are rounded for a cache: sequence b is
+ * the rows start_dev[b] .. start_dev[b+1] - 1 of q, k and v (start_dev never decreases; NULL: one sequence of all rows),
+ * and its row i sees its rows t <= i, with a window > 0 only those with t > i - window.  Head h reads key/value head h / (heads / kv_heads).
+ *   out = sum over seen t of softmax(scale * q.k_t) v_t,   sums = log sum exp(scale * q.k_t)
+ * Scores are sums in 32 bits of exact products.  Weights go into their products in the tensors' type (bf16: 8 bits, as the results have;
+ * fp16: 11 bits), and a row is divided by the sum of what went in; blocks of fp16 rows in which weights below 2^-24 of a row's
+ * largest may matter are done again with 16 bits, whatever a weight's size.  Weights go up to 2^8 (bf16) and 2^15 (fp16) before a row's largest is
+ * taken down, and the sum is divided last: where it passes 2^128 on the way, results are infinite.
+ * What lies in rows that a row does not see has no effect on it, NaN included (but it may change its last place, where values
+ * that are not finite make a block of rows be done again).
+ * Rows that are no sequence's are left as they were, in out and sums.  head_dim: a multiple of 32 up to 256; tokens * heads <= 2^30, 32768 heads to a
+ * key/value head (MACKO_E_UNSUPPORTED otherwise).  out must not overlap q, k or v.  One launch, no workspace. */
+typedef struct macko_prompt_args {
+  int64_t tokens;
+  int32_t heads, kv_heads, head_dim, type, batch;
+  const void* q_dev;
+  int64_t q_token, q_head;
+  const void* k_dev;
+  int64_t k_token, k_head;
+  const void* v_dev;
+  int64_t v_token, v_head;
+  void* out_dev;
+  int64_t out_token, out_head;
+  float* sums_dev;              /* [tokens][heads], or NULL */
+  const int32_t* start_dev;     /* [batch + 1], or NULL */
+  int32_t window;
+  int64_t longest;              /* rows of one sequence at most: sizes the launch, too small costs time, not correctness */
+  float scale;
+} macko_prompt_args_t;
+MACKO_API int macko_prompt_attention(const macko_prompt_args_t* args, void* stream);
+
 /* ---- housekeeping ---------------------------------------------------------- */
 
 /* Waits until the device is idle if the handle owns device memory (that of the GPU encoder). */

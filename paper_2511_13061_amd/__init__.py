@@ -33,4 +33,4 @@ from .binding import (  # noqa: F401
     wrap_device,
     wrap_device_fp8,
 )
-from .kv import KvCache, KvCache8, rope_table, rotate  # noqa: F401,E402
+from .kv import KvCache, KvCache8, attend_prompt, rope_table, rotate  # noqa: F401,E402

@@ -22,7 +22,7 @@ EXPORTED_SYMBOLS = [
     "macko_last_hip_error", "macko_set_tuning", "macko_get_tuning",
     "macko_kv_cache_bytes", "macko_rope_table", "macko_rotate", "macko_kv_append", "macko_kv_read",
     "macko_kv_attention_workspace", "macko_kv_attention", "macko_kv8_cache_bytes", "macko_kv8_append", "macko_kv8_read",
-    "macko_kv8_attention_workspace", "macko_kv8_attention",
+    "macko_kv8_attention_workspace", "macko_kv8_attention", "macko_prompt_attention",
 ]
 
 
@@ -161,7 +161,7 @@ def load_library():
         native.bind(*[ctypes.cast(f, vp).value for f in (
             lib.macko_spmv, lib.macko_spmm, lib.macko_decode_device, lib.macko_rotate, lib.macko_kv_append, lib.macko_kv_read,
             lib.macko_kv_attention_workspace, lib.macko_kv_attention, lib.macko_kv8_append, lib.macko_kv8_read,
-            lib.macko_kv8_attention_workspace, lib.macko_kv8_attention)])
+            lib.macko_kv8_attention_workspace, lib.macko_kv8_attention, lib.macko_prompt_attention)])
         _native = native
     _lib = lib
     return lib

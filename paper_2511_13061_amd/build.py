@@ -11,8 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmacko.so")
 BINDING = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["macko_host.cpp", "macko_spmv.hip", "macko_gemv.hip", "macko_encode_gpu.hip", "macko_spmm.hip", "macko_spmm_tile.hip", "macko_decode_gpu.hip", "macko_kv.hip", "macko_kv_attention.hip", "macko_kv_prompt.hip", "macko_kv8.hip", "macko_kv8_attention.hip"]
-HEADERS = ["macko_internal.h", "macko_device.h", "macko_plan.h", "macko_decode.h", "macko_kv.h", "macko_kv_attention.h", "macko_kv8.h", "macko_kv8_attention.h"]
+SOURCES = ["macko_host.cpp", "macko_spmv.hip", "macko_gemv.hip", "macko_encode_gpu.hip", "macko_spmm.hip", "macko_spmm_tile.hip", "macko_decode_gpu.hip", "macko_kv.hip", "macko_kv_attention.hip", "macko_kv_prompt.hip", "macko_kv8.hip", "macko_kv8_attention.hip", "macko_kv8_prompt.hip", "macko_prompt.hip"]
+HEADERS = ["macko_internal.h", "macko_device.h", "macko_plan.h", "macko_decode.h", "macko_kv.h", "macko_kv_attention.h", "macko_kv8.h", "macko_kv8_attention.h", "macko_rows.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -38,6 +38,7 @@ decltype(&macko_kv8_append) g_append8 = nullptr;
 decltype(&macko_kv8_read) g_read8 = nullptr;
 decltype(&macko_kv8_attention_workspace) g_workspace8 = nullptr;
 decltype(&macko_kv8_attention) g_attention8 = nullptr;
+decltype(&macko_prompt_attention) g_prompt = nullptr;
 
 // A forked child may not use its parent's device.  PyTorch's Python calls refuse that with an error, the C++ calls below do not:
 // in a child the functions serve nothing, and the general way says what there is to say.
@@ -408,10 +409,57 @@ PyObject* kv8_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// attend_prompt(q, k, v, start, longest or None, scale or None, window, sums, out)
+PyObject* attend_prompt(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments");
+  const Given q(args[0]), k(args[1]), v(args[2]), start(args[3]), out(args[8]);
+  const int64_t longest = args[4] == Py_None ? -1 : PyLong_AsLongLong(args[4]), window = PyLong_AsLongLong(args[6]);
+  const double scale = args[5] == Py_None ? 0.0 : PyFloat_AsDouble(args[5]);
+  const bool sums = PyObject_IsTrue(args[7]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!g_prompt || g_forked || !q.t || !k.t || !v.t || !start.fine || !out.fine || q.t->dim() != 3 || k.t->dim() != 3) Py_RETURN_NONE;
+  const c10::DeviceIndex device = c10::hip::current_device();
+  const int64_t tokens = q.t->size(0), heads = q.t->size(1), dim = q.t->size(2), kv_heads = k.t->size(1);
+  const at::ScalarType scalar = q.t->scalar_type();
+  macko_prompt_args_t a{};
+  a.type = type_of(*q.t);
+  if (a.type < 0 || tokens == 0 || heads > INT32_MAX || kv_heads > INT32_MAX || dim > INT32_MAX || window < 0 || window > INT32_MAX || longest < (args[4] == Py_None ? -1 : 0) ||
+      !heads_fit(*q.t, tokens, heads, dim, scalar, device) || !heads_fit(*k.t, tokens, kv_heads, dim, scalar, device) || !heads_fit(*v.t, tokens, kv_heads, dim, scalar, device) ||
+      (start.t && (start.t->dim() != 1 || start.t->size(0) < 1 || start.t->size(0) > INT32_MAX || !ints_fit(*start.t, start.t->size(0), device))) ||
+      (out.t && !made_fits(*out.t, tokens, heads, dim, scalar, device)))
+    Py_RETURN_NONE;
+  a.tokens = tokens, a.heads = (int32_t)heads, a.kv_heads = (int32_t)kv_heads, a.head_dim = (int32_t)dim;
+  a.q_dev = q.t->data_ptr(), a.q_token = q.t->stride(0), a.q_head = q.t->stride(1);
+  a.k_dev = k.t->data_ptr(), a.k_token = k.t->stride(0), a.k_head = k.t->stride(1);
+  a.v_dev = v.t->data_ptr(), a.v_token = v.t->stride(0), a.v_head = v.t->stride(1);
+  if (start.t) a.start_dev = static_cast<const int32_t*>(start.t->data_ptr()), a.batch = (int32_t)(start.t->size(0) - 1);
+  a.window = (int32_t)window;
+  a.longest = longest < 0 ? tokens : longest;
+  a.scale = args[5] == Py_None ? (float)(1.0 / std::sqrt((double)dim)) : (float)scale;
+  at::Tensor made, total;
+  int status;
+  {
+    pybind11::gil_scoped_release unlocked;
+    if (!out.t) made = made_heads(tokens, heads, dim, *q.t);
+    const at::Tensor& y = out.t ? *out.t : made;
+    a.out_dev = y.data_ptr(), a.out_token = y.stride(0), a.out_head = y.stride(1);
+    if (sums) {
+      total = at::empty({tokens, heads}, q.t->options().dtype(at::kFloat));
+      a.sums_dev = static_cast<float*>(total.data_ptr());
+    }
+    status = g_prompt(&a, c10::hip::getCurrentHIPStream().stream());
+  }
+  if (sums) return two(status, made, args[8], total, Py_None);
+  return result(status, made, args[8]);
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses of macko_spmv, macko_spmm, macko_decode_device, macko_rotate, macko_kv_append, macko_kv_read, macko_kv_attention_workspace,
-// macko_kv_attention, macko_kv8_append, macko_kv8_read, macko_kv8_attention_workspace, macko_kv8_attention)
+// macko_kv_attention, macko_kv8_append, macko_kv8_read, macko_kv8_attention_workspace, macko_kv8_attention,
+// macko_prompt_attention)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  constexpr int kCalls = 12;
+  constexpr int kCalls = 13;
   if (n != kCalls) return PyErr_Format(PyExc_TypeError, "%d arguments", kCalls);
   void* p[kCalls];
   for (int i = 0; i < kCalls; ++i) p[i] = PyLong_AsVoidPtr(args[i]);
@@ -429,12 +477,14 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   g_read8 = reinterpret_cast<decltype(g_read8)>(p[9]);
   g_workspace8 = reinterpret_cast<decltype(g_workspace8)>(p[10]);
   g_attention8 = reinterpret_cast<decltype(g_attention8)>(p[11]);
+  g_prompt = reinterpret_cast<decltype(g_prompt)>(p[12]);
   Py_RETURN_NONE;
 }
 
 #define MACKO_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MACKO_FAST(spmv), MACKO_FAST(spmm), MACKO_FAST(decode_device), MACKO_FAST(rotate), MACKO_FAST(kv_append), MACKO_FAST(kv_read), MACKO_FAST(kv_attend),
-                         MACKO_FAST(kv8_append), MACKO_FAST(kv8_read), MACKO_FAST(kv8_attend), MACKO_FAST(bind), {nullptr, nullptr, 0, nullptr}};
+                         MACKO_FAST(kv8_append), MACKO_FAST(kv8_read), MACKO_FAST(kv8_attend), MACKO_FAST(attend_prompt),
+                         MACKO_FAST(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

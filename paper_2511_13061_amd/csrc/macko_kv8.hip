@@ -119,20 +119,6 @@ __device__ inline void finish(const AppendArgs& a, Packed8 raw, const uint16_t* 
   }
 }
 
-// The sequence whose rows hold `row`: the last one that starts there or before (`batch`: behind them all, -1: in front).  64 starts at a time.
-__device__ inline int sequence_at(const int32_t* start, int batch, int row, int lane) {
-  int lo = 0, count = batch + 1;                          // the last of [lo, lo + count) that is at most `row`
-  while (count > 1) {
-    const int step = (count + 63) / 64, at = min(lane * step, count - 1);
-    const uint64_t before = __ballot(start[lo + at] <= row && lane * step < count);
-    if (before == 0) return -1;
-    const int steps = __popcll(before) - 1;
-    lo += steps * step;
-    count = min(step, count - steps * step);
-  }
-  return lo;
-}
-
 // A wavefront either turns queries (groups of LT lanes take BUNDLE heads of a token) or stores: it takes the blocks of 16 places of a sequence whose first new
 // token is one of its `rows` rows, for keys or values of one head or, where a block takes fewer lanes, of several.  In a block lane (t, l) has 8 channels of TPL
 // places, so that the values' words, 4 places of a channel, are made without another lane; all of a block's new tokens are there at once, and the largest

@@ -5,8 +5,7 @@
 //   scores   S^T = K Q^T in the queries' type, which holds every code exactly; products of 16 bits, sums of 32.  A block's power of two goes onto its codes (bf16, where
 //            it changes nothing but the exponent) or onto its scores (fp16, whose exponents do not reach as far).
 //   softmax  running maximum and sum in 32 bits.  Column r of S^T is row r, so a lane holds 8 scores of one row; the running maximum moves only when a score
-//            is more than 2^8 above it, and only then do lanes talk to each other.  The sum carries what its roundings left out: a token that is far ahead of very
-//            many others would lose them, step by step.
+//            is more than 2^8 above it, and only then do lanes talk to each other.  The sum is taken anew every 32 steps.
 //   values   O^T += V^T P^T in bf16, which holds codes exactly with any of the scales; weights go in as two bf16 parts (16 bits).  The lanes of S^T that hold a
 //            token's weights are those that P^T needs, and a lane's 4 tokens of a channel are a word of the cache: nothing moves between lanes.
 // The four wavefronts of a workgroup take turns along the tokens and join their sums in LDS; long sequences are split over workgroups
@@ -25,15 +24,7 @@ struct Tile8 {
   uint32_t scale[2];
 };
 
-template <int W>
-__device__ inline void load_words(uint32_t* to, const uint8_t* from) {
-  typedef uint32_t Words __attribute__((ext_vector_type(W)));
-  const Words w = *reinterpret_cast<const Words*>(from);
-#pragma unroll
-  for (int i = 0; i < W; ++i) to[i] = w[i];
-}
-
-constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? (ng <= 2 ? 3 : 2) : ng <= 2 ? 4 : ng <= 4 ? 2 : 1; }
+constexpr int waves_wanted(int ng, int rt) { return rt == 2 ? (ng == 1 ? 3 : 2) : ng == 1 ? 4 : ng == 2 ? 3 : ng <= 4 ? 2 : 1; }
 
 template <int NG, bool BF, int RT>
 __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_kernel(const Launch8 args) {
@@ -45,6 +36,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
   float* const lds_sum = lds_max + kWaves * 16;
   int* const lds_place = reinterpret_cast<int*>(lds_sum + kWaves * 16);                 // [R]
   uint32_t* const lds_spoilt = reinterpret_cast<uint32_t*>(lds_place + R);              // [R][NG]: channels in which a row sees what is not a number
+  // [RT][thread]: a lane's sum up to the last 32 steps, out of the registers' way.  A token that is far ahead of very many others would lose them, step by step.
+  float* const lds_whole = reinterpret_cast<float*>(lds_spoilt + R * NG);
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x, split = g.splits == 1 ? 0 : g.row_blocks == 1 ? (int)blockIdx.z : (int)blockIdx.z / g.row_blocks, row_block = (int)blockIdx.z - split * g.row_blocks;
@@ -54,8 +47,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
   const int32_t* const table = a.tables + b * a.table_stride;
   const int block_bits = a.pool.page_bits - kBlockBits;  // log2 of a page's blocks
   // Weights are 2^(score * unit - maximum); the scale's sign goes into the queries, so that the largest score has the largest weight.
-  const float unit = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;
-  const float lift = fminf(kLift / unit, 0x1p127f);      // finite: nothing is above -infinity by an infinity, and the first maximum would never be taken
+  const float unit = scalar(a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f);
+  const float lift = scalar(fminf(kLift / unit, 0x1p127f));      // finite: nothing is above -infinity by an infinity, and the first maximum would never be taken
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : 0xFFFFFFFFu;
   const uint32_t reach = a.window ? (uint32_t)a.window : 0x7FFFFFFFu;
 
@@ -103,13 +96,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
     }
 
     // Queries as the operand: a lane has the channels that a lane of the keys has.
-    int place[RT];                                        // of a row's query: it sees the tokens t with 0 <= place - t < reach
     V4i q[RT][NG];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int row = first_row + rt * 16 + n, query = rows.query_of(a, g, row);
       const bool there = row < seq.rows;
-      place[rt] = there ? seq.length - seq.queries + query : -1;
       const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + query) * a.q_token + (int64_t)(head * a.shared + row - query * a.shared) * a.q_head;
 #pragma unroll
       for (int s = 0; s < NG; ++s) {
@@ -118,20 +109,28 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[rt][s][i] = (int)((raw[i] ^ flip) & keep);
       }
-      if (wave == 0 && j == 0) lds_place[rt * 16 + n] = place[rt];
+      // of a row's query: it sees the tokens t with 0 <= place - t < reach
+      if (wave == 0 && j == 0) lds_place[rt * 16 + n] = there ? seq.length - seq.queries + query : -1;
     }
     for (int i = threadIdx.x; i < R * NG; i += 64 * kWaves) lds_spoilt[i] = 0;
     __syncthreads();
 
-    float top[RT], sum[RT], rest[RT];                     // rest: what the sum's roundings left out
+    float top[RT], sum[RT];
     V4f out[RT][2 * NG];
+    auto gather = [&] {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        lds_whole[rt * 64 * kWaves + later(threadIdx.x)] += sum[rt];
+        sum[rt] = 0.f;
+      }
+    };
     auto step = [&](Tile8<NG>& t, int at, bool careful) {
       const bool masked = at < span.all_lo || at + kTile > span.all_hi;
       V4i p_hi[RT], p_lo[RT];
       float x[RT][8];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float key_unit = power_of(t.scale[u] & 255u);
+        const float key_unit = scalar(power_of((uint32_t)__builtin_amdgcn_readfirstlane((int)t.scale[u]) & 255u));
         V4f s[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt] = V4f{0.f, 0.f, 0.f, 0.f};
@@ -149,10 +148,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         if (masked) {
+          const int place = lds_place[rt * 16 + n];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int token = at + (i >> 2) * 16 + j * 4 + (i & 3);
-            if ((uint32_t)(place[rt] - token) >= reach) x[rt][i] = -INFINITY;
+            if ((uint32_t)(place - token) >= reach) x[rt][i] = -INFINITY;
           }
         }
         const float* const y = x[rt];
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
           const float by = to == top[rt] ? 1.f : __builtin_amdgcn_exp2f((top[rt] - to) * unit);
           top[rt] = to;
           sum[rt] *= by;
-          rest[rt] *= by;
+          lds_whole[rt * 64 * kWaves + later(threadIdx.x)] *= by;
 #pragma unroll
           for (int c = 0; c < 2 * NG; ++c) out[rt][c] *= by;
         }
@@ -175,9 +175,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
           weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], unit, base));
           more = i == 0 ? weight[0] : more + weight[i];
         }
-        const float lacking = more + rest[rt], now = sum[rt] + lacking;
-        rest[rt] = lacking - (now - sum[rt]);
-        sum[rt] = now;
+        sum[rt] += more;                                  // `more`: of the step alone, for the same reason as lds_whole
         parts_of<false>(weight, p_hi[rt], p_lo[rt]);
       }
       if (careful || at < span.first || at + kTile > span.hi) {
@@ -198,6 +196,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
 #pragma unroll 1
               for (int i = 0; i < 4; ++i) {
                 if (!(odd >> 8 * i & 1)) continue;
+#pragma unroll 1
                 for (int r = 0; r < R; ++r)
                   if ((uint32_t)(lds_place[r] - (token + i)) < reach) atomicOr(lds_spoilt + r * NG + (channel >> 5), 1u << (channel & 31));
               }
@@ -206,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
           }
         }
       }
-      const float unit0 = power_of(t.scale[0] >> 8), unit1 = power_of(t.scale[1] >> 8);
+      const float unit0 = scalar(power_of((uint32_t)__builtin_amdgcn_readfirstlane((int)t.scale[0]) >> 8)), unit1 = scalar(power_of((uint32_t)__builtin_amdgcn_readfirstlane((int)t.scale[1]) >> 8));
 #pragma unroll
       for (int w = 0; w < 2 * NG; ++w) {
         const V4i v = {pair_of<true>(t.value[0][w], unit0, false), pair_of<true>(t.value[0][w], unit0, true), pair_of<true>(t.value[1][w], unit1, false),
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         top[rt] = -INFINITY;
-        sum[rt] = rest[rt] = 0.f;
+        sum[rt] = lds_whole[rt * 64 * kWaves + later(threadIdx.x)] = 0.f;
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c) out[rt][c] = V4f{0.f, 0.f, 0.f, 0.f};
       }
@@ -238,6 +237,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
           if (++slot == 32) {
             look_up(next);
             slot = 0;
+            gather();
           }
           load(t, next, slot);
         };
@@ -265,10 +265,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
       if (!__any(one_of != one_of)) break;
     }
 
+    // What the results need of the arguments is read again here, rather than kept in registers through the steps.
+    typedef const __attribute__((address_space(4))) Launch8* Launch8Ptr;
+    Launch8Ptr e = (Launch8Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(e));
     const int thread = later(threadIdx.x), row16 = thread & 15, quad = thread >> 4 & 3;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float total_of_row = sum[rt] + rest[rt];
+      float total_of_row = sum[rt] + lds_whole[rt * 64 * kWaves + thread];
       total_of_row += __shfl_xor(total_of_row, 16);
       total_of_row += __shfl_xor(total_of_row, 32);
       if (bad) total_of_row = NAN;
@@ -304,25 +308,25 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
         const uint32_t spoilt = lds_spoilt[(rt * 16 + r) * NG + (channel >> 5)] >> (channel & 31);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = spoilt >> i & 1 ? NAN : o[i];
-        const int query = rows.query_of(a, g, row), h = head * a.shared + row - query * a.shared;
+        const int query = rows.query_of(a, g, row), h = head * e->a.shared + row - query * e->a.shared;
         const int64_t token = seq.first + query;
         if (span.used > 1) {
-          const int64_t part = (token * a.heads + h) * g.splits + split;
-          *reinterpret_cast<V4f*>(g.parts + part * D + channel) = o;
+          const int64_t part = (token * e->a.heads + h) * e->g.splits + split;
+          *reinterpret_cast<V4f*>(e->g.parts + part * D + channel) = o;
           if (channel == 0) {
-            float* const ms = g.parts + a.tokens * a.heads * g.splits * D + part * 2;
+            float* const ms = e->g.parts + e->a.tokens * e->a.heads * e->g.splits * D + part * 2;
             ms[0] = most;
             ms[1] = total;
-            if (split == 0) used_splits(a, g)[token * a.heads + h] = span.used;
+            if (split == 0) used_splits(e->a, e->g)[token * e->a.heads + h] = span.used;
           }
           continue;
         }
         const float r1 = total == 0.f ? 0.f : 1.f / total;
         typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(2)));
-        *reinterpret_cast<Pair*>(reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + h * a.out_head + channel) =
+        *reinterpret_cast<Pair*>(reinterpret_cast<uint16_t*>(e->a.out) + token * e->a.out_token + h * e->a.out_head + channel) =
             Pair{pack2<BF>(o[0] * r1, o[1] * r1), pack2<BF>(o[2] * r1, o[3] * r1)};
-        if (g.splits > 1 && channel == 0) used_splits(a, g)[token * a.heads + h] = 1;
-        if (a.sums && channel == 0) a.sums[token * a.heads + h] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+        if (e->g.splits > 1 && channel == 0) used_splits(e->a, e->g)[token * e->a.heads + h] = 1;
+        if (e->a.sums && channel == 0) e->a.sums[token * e->a.heads + h] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
       }
       __syncthreads();
     }
@@ -332,13 +336,17 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
 // Two tiles of rows share the decoded values where there are more rows than one has.
 int row_tiles(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > 16 && a.pool.dim <= 128 ? 2 : 1; }
 
+// Rows of a sequence up to which the kernel for few rows takes a call.
+constexpr int kFewRows = 64;
+
 Grid grid_of(const KvAttention& a) {
   Grid g{};
   g.unit = kWaves * kTile;
   g.shared_inverse = a.shared == 1 ? 0u : (uint32_t)(((uint64_t{1} << 32) + a.shared - 1) / a.shared);
   const int64_t unit = g.unit, most_rows = (int64_t)a.most_queries * a.shared;
   const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
-  g.rows = 16 * row_tiles(a);
+  const bool many = tuning().attention_kernel ? tuning().attention_kernel == 2 : most_rows > kFewRows;
+  g.rows = many ? 32 * kWaves : 16 * row_tiles(a);
   const int64_t row_blocks = (most_rows + g.rows - 1) / g.rows, others = (int64_t)a.batch * a.pool.heads * row_blocks, units = (longest + unit - 1) / unit;
   int64_t splits = std::max<int64_t>(1, std::min({(int64_t)device_cu_count() * 2 / others, units / 4, (int64_t)kMostSplits}));
   if (tuning().attention_parts > 0) splits = std::min({tuning().attention_parts, units, (int64_t)kMostSplits});
@@ -352,7 +360,7 @@ Grid grid_of(const KvAttention& a) {
 
 template <int NG, bool BF, int RT>
 int launch_of(const Launch8& l, hipStream_t stream) {
-  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + 2 * kWaves * 16 + 16 * RT + 16 * RT * NG);
+  constexpr int lds = 4 * (kWaves * 16 * (32 * NG + 4) + 2 * kWaves * 16 + 16 * RT + 16 * RT * NG + RT * 64 * kWaves);
   const KvAttention& a = l.a;
   if (lds > 64 * 1024) MACKO_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention8_kernel<NG, BF, RT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   hipLaunchKernelGGL((attention8_kernel<NG, BF, RT>), dim3((unsigned)a.pool.heads, (unsigned)a.batch, (unsigned)(l.g.row_blocks * l.g.splits)), dim3(64 * kWaves), lds, stream, l);
@@ -398,7 +406,7 @@ int64_t kv8_attention_workspace(const KvAttention& a) {
 int launch_kv8_attention(const Kv8Attention& a, float* workspace, hipStream_t stream) {
   Launch8 l{a.a, grid_of(a.a), a.scales};
   l.g.parts = workspace;
-  const int status = launch_width(l, stream);
+  const int status = l.g.rows >= 64 ? launch_kv8_rows(l, stream) : launch_width(l, stream);
   return status == MACKO_OK && l.g.splits > 1 ? launch_join(a.a, l.g, stream) : status;
 }
 

@@ -1,6 +1,6 @@
-"""Heads between a decoder layer's products: rotation, the paged 4-bit key/value cache, attention over it.
+"""Heads between a decoder layer's products: rotation, paged key/value caches in 4 and in 8 bits, attention over them, and of a prompt over its own keys and values.
 
-Same names as the C ABI (``include/macko.h``, "keys and values in 4 bits"), argument checks and marshalling only.  For inference: results have no
+Same names as the C ABI (``include/macko.h``, from "between the products of a decoder layer" on), argument checks and marshalling only.  For inference: results have no
 gradient, also where an argument requires one.
 """
 from __future__ import annotations
@@ -48,6 +48,12 @@ class _CAttention(ctypes.Structure):
                 ("scale", _f32)]
 
 
+class _CPrompt(ctypes.Structure):
+    _fields_ = [("tokens", _i64), ("heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("type", _i32), ("batch", _i32), ("q", _vp), ("q_token", _i64),
+                ("q_head", _i64), ("k", _vp), ("k_token", _i64), ("k_head", _i64), ("v", _vp), ("v_token", _i64), ("v_head", _i64), ("out", _vp),
+                ("out_token", _i64), ("out_head", _i64), ("sums", _vp), ("start", _vp), ("window", _i32), ("longest", _i64), ("scale", _f32)]
+
+
 def _declare(lib) -> None:
     """Argument types of the calls of this file (load_library)."""
     cp = ctypes.POINTER(_CCache)
@@ -68,6 +74,7 @@ def _declare(lib) -> None:
     lib.macko_kv8_attention_workspace.argtypes = [cp, ctypes.POINTER(_CAttention)]
     lib.macko_kv8_attention_workspace.restype = _i64
     lib.macko_kv8_attention.argtypes = [cp, ctypes.POINTER(_CAttention), _vp, _i64, _vp]
+    lib.macko_prompt_attention.argtypes = [ctypes.POINTER(_CPrompt), _vp]
 
 
 def _type_of(x) -> int:
@@ -190,6 +197,42 @@ def rotate(x, positions, table, weight=None, eps=1e-6, interleaved=False, out=No
         dst = _made_heads(out, "out", x.shape, x)
         _check(load_library().macko_rotate(x.shape[0], x.shape[1], x.shape[2], kind, *src, ctypes.byref(r), w, *dst, _stream_ptr(stream)), "macko_rotate")
     return out
+
+
+def attend_prompt(q, k, v, start=None, longest=None, scale=None, window=0, sums=False, out=None, stream=None):
+    """macko_prompt_attention: causal attention of packed sequences, q [tokens, heads, head_dim] over k and v [tokens, kv_heads, head_dim] of the same type.
+
+    start: int32 [sequences + 1], the rows that are each sequence's; None: all rows are one.  longest: a bound on the rows of one sequence, all rows unless
+    given.  scale: head_dim ** -0.5 unless given.  Returns out, or (out, sums) with sums = True: float32 [tokens, heads], the logarithm of each row's
+    sum, to join results with those over a cached prefix."""
+    if stream is None and binding._native is not None:
+        y = binding._native.attend_prompt(q, k, v, start, longest, scale, window, sums, out)
+        if y is not None:
+            return _made(y, "macko_prompt_attention")
+    torch = _need_torch()
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q must be [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim]")
+    kind, shape = _type_of(q), tuple(q.shape)
+    held = (shape[0], k.shape[1], shape[2])
+    a = _CPrompt(*shape[:2], held[1], shape[2], kind)
+    a.q, a.q_token, a.q_head = _heads(q, "q", shape)
+    a.k, a.k_token, a.k_head = _heads(k, "k", held, q)
+    a.v, a.v_token, a.v_head = _heads(v, "v", held, q)
+    if start is not None:
+        a.batch = start.shape[0] - 1 if start.dim() == 1 else -1
+        a.start = _ints(start, "start", (a.batch + 1,), q)
+    a.window = _whole(window, "window")
+    a.longest = shape[0] if longest is None else _whole(longest, "longest", 64)
+    a.scale = 1.0 / math.sqrt(shape[2]) if scale is None else scale
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        a.out, a.out_token, a.out_head = _made_heads(out, "out", shape, q)
+        total = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if sums else None
+        if sums:
+            a.sums = total.data_ptr()
+        _check(load_library().macko_prompt_attention(ctypes.byref(a), _stream_ptr(stream)), "macko_prompt_attention")
+    return (out, total) if sums else out
 
 
 def _read(cache, name, slots, dtype, k_out, v_out, stream):
