@@ -28,10 +28,11 @@ struct AppendArgs {
   const int32_t *tables, *lengths, *start;
   int64_t table_stride;
   Kv8Pool pool;
-  int64_t tokens, q_items, q_waves, waves;       // of queries: bundles of heads; wavefronts of queries, and of the launch
-  int32_t table_width, batch, heads, bundles, dim, rot, interleaved;
-  int32_t rows;              // of a wavefront that stores: it takes the blocks that begin in them
-  int32_t pair_waves;        // wavefronts that share a token's keys and values out
+  int64_t tokens;
+  int32_t q_groups;          // append_kernel: workgroups that share a token's queries out
+  int32_t table_width, batch, heads, dim, rot, interleaved;
+  int32_t rows;              // that are looked for blocks together
+  int32_t groups;            // wavefronts (append_kernel) or workgroups (blocks_kernel) that share the heads' keys out, and as many their values
   float eps;
 };
 
@@ -55,19 +56,15 @@ struct Turn {
   int other;                 // the lane that holds the other channels of this one's pairs
   bool turned, placed;
 };
-__device__ inline Turn turn_of(const AppendArgs& a, int64_t token, int lane) {
+// `row`: the cosines, then the sines, of the token's position.
+__device__ inline Turn turn_by(const AppendArgs& a, const float* row, bool placed, int lane) {
   Turn t;
   const int half = a.rot >> 4;                            // lanes of half a turned part
   t.other = lane >= 2 * half ? lane : lane < half ? lane + half : lane - half;
-  t.placed = true;
-  int64_t at = 0;
-  if (a.rot > 0) {
-    at = a.positions[token];
-    t.placed = at >= 0 && at < a.table_rows;
-  }
-  t.turned = t.placed && lane < 2 * half;
+  t.placed = placed;
+  t.turned = placed && lane < 2 * half;
   if (t.turned) {
-    const float* const row = a.table + at * a.rot + (a.interleaved ? lane * 4 : (lane < half ? lane : t.other) * 8);
+    row += a.interleaved ? lane * 4 : (lane < half ? lane : t.other) * 8;
     *reinterpret_cast<V4*>(t.c) = *reinterpret_cast<const V4*>(row);
     *reinterpret_cast<V4*>(t.s) = *reinterpret_cast<const V4*>(row + a.rot / 2);
     if (!a.interleaved) {
@@ -78,6 +75,10 @@ __device__ inline Turn turn_of(const AppendArgs& a, int64_t token, int lane) {
     }
   }
   return t;
+}
+__device__ inline Turn turn_of(const AppendArgs& a, int64_t token, int lane) {
+  const int64_t at = a.rot > 0 ? a.positions[token] : 0;
+  return turn_by(a, a.table + at * a.rot, a.rot == 0 || (at >= 0 && at < a.table_rows), lane);
 }
 
 // 8 channels of a head, normalised and turned; NaN where the token's position lies outside the table.
@@ -119,173 +120,293 @@ __device__ inline void finish(const AppendArgs& a, Packed8 raw, const uint16_t* 
   }
 }
 
-// A wavefront either turns queries (groups of LT lanes take BUNDLE heads of a token) or stores: it takes the blocks of 16 places of a sequence whose first new
-// token is one of its `rows` rows, for keys or values of one head or, where a block takes fewer lanes, of several.  In a block lane (t, l) has 8 channels of TPL
-// places, so that the values' words, 4 places of a channel, are made without another lane; all of a block's new tokens are there at once, and the largest
-// magnitude takes one round of exchanges.  Only where the byte of scale grows are the block's earlier tokens read at all.
-template <bool BF, int LB, int BUNDLE>
-__global__ __launch_bounds__(kBlock) void append_kernel(const AppendArgs a) {
-  constexpr int LT = 1 << LB, TG = LT <= 16 ? 4 : 2, GROUP = LT * TG, TPL = 16 / TG, PAIRS = kWave / GROUP;
-  const int lane64 = threadIdx.x & 63, lane = lane64 & (LT - 1);
-  const bool mine = lane * 8 < a.dim;
-  for (int64_t wave = (int64_t)blockIdx.x * (kBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wave < a.waves; wave += (int64_t)gridDim.x * (kBlock / kWave)) {
-    if (wave < a.q_waves) {
-      const int64_t item = wave * (kWave / LT) + (lane64 >> LB), token = min(item / a.bundles, a.tokens - 1);
-      const int head = (int)(item - item / a.bundles * a.bundles) * BUNDLE;
-      const bool there = item < a.q_items;
-      Packed8 raw[BUNDLE];
-#pragma unroll
-      for (int i = 0; i < BUNDLE; ++i) {
-        raw[i] = Packed8{0, 0, 0, 0};
-        if (there && mine && head + i < a.heads) raw[i] = *reinterpret_cast<const Packed8Any*>(a.q + token * a.q_token + (head + i) * a.q_head + lane * 8);
-      }
-      const Turn t = turn_of(a, token, lane);
-#pragma unroll
-      for (int i = 0; i < BUNDLE; ++i) {
-        float y[8];
-        finish<BF, LT>(a, raw[i], a.q_weight, t, lane, y);
-        if (there && mine && head + i < a.heads) *reinterpret_cast<Packed8Any*>(a.out + token * a.out_token + (head + i) * a.out_head + lane * 8) = pack8<BF>(y);
-      }
+// The next block of 16 places of a sequence that a call's rows from w.row on begin: its new tokens are the places [first, last), the rows row0 + place.
+struct Walk {
+  int row, end, b;
+};
+struct NewTokens {
+  int row0, first, last;
+  int b, place;              // the sequence, the block's first token in it
+};
+// The page that a block lies in; < 0: none.
+__device__ inline int page_of(const AppendArgs& a, const NewTokens& n) {
+  const int index = n.place >> a.pool.page_bits, page = index < a.table_width ? constant(a.tables + n.b * a.table_stride + index) : -1;
+  return page >= 0 && page < a.pool.pages ? page : -1;
+}
+__device__ inline Walk walk_of(const AppendArgs& a, int64_t chunk, int lane64) {
+  Walk w{(int)(chunk * a.rows), (int)min((chunk + 1) * a.rows, a.tokens), 0};
+  w.b = a.start ? sequence_at(a.start, a.batch, w.row, lane64) : w.row;
+  if (w.b < 0) w.b = 0, w.row = min(max(a.start[0], 0), w.end);
+  return w;
+}
+__device__ inline bool next_block(const AppendArgs& a, Walk& w, NewTokens& n) {
+  while (w.row < w.end && w.b < a.batch) {
+    const int from = a.start ? min(max(constant(a.start + w.b), 0), (int)a.tokens) : w.row, to = a.start ? min(max(constant(a.start + w.b + 1), 0), (int)a.tokens) : w.row + 1;
+    if (w.row >= to) {                                    // the sequence's rows are over, or it has none
+      ++w.b;
       continue;
     }
-    const int64_t unit = wave - a.q_waves, chunk = unit / a.pair_waves;
-    const int pair = (int)(unit - chunk * a.pair_waves) * PAIRS + lane64 / GROUP;        // keys' heads, then values'
-    const bool there = pair < 2 * a.pool.heads, value = pair >= a.pool.heads && there;
-    const int head = there ? pair - (value ? a.pool.heads : 0) : 0;
-    const int first_place = (lane64 / LT) % TG * TPL;
-    const int row_end = (int)min((chunk + 1) * a.rows, a.tokens);
-    int row = (int)(chunk * a.rows);
-    int b = a.start ? sequence_at(a.start, a.batch, row, lane64) : row;
-    if (b < 0) b = 0, row = min(max(a.start[0], 0), row_end);
-    while (row < row_end && b < a.batch) {
-      const int from = a.start ? min(max(a.start[b], 0), (int)a.tokens) : row, to = a.start ? min(max(a.start[b + 1], 0), (int)a.tokens) : row + 1;
-      if (row >= to) {                                    // the sequence's rows are over, or it has none
-        ++b;
-        continue;
-      }
-      const int length = min(max(a.lengths[b], 0), kMostTokens);
-      int place = length - (to - row);
-      if (place < 0) {                                    // more rows than tokens: these have no place
-        row = min(to, row - place);
-        if (row >= to) ++b;
-        continue;
-      }
-      const int first = place & 15, last = min(16, first + (to - row));      // places of the block that are new
-      const int row0 = row - first, sequence = b;
-      const bool begins = first == 0 || row == from;
-      row = row0 + last;
-      if (row >= to) ++b;
-      if (!begins) continue;                              // the block begins in rows before these
-      const int index = place >> a.pool.page_bits;
-      const int page = index < a.table_width ? a.tables[sequence * a.table_stride + index] : -1;
-      if (page < 0 || page >= a.pool.pages) continue;
+    const int place = min(max(constant(a.lengths + w.b), 0), kMostTokens) - (to - w.row);
+    if (place < 0) {                                      // more rows than tokens: these have no place
+      w.row = min(to, w.row - place);
+      continue;
+    }
+    n.first = place & 15, n.last = min(16, n.first + (to - w.row));
+    n.row0 = w.row - n.first;
+    const bool begins = n.first == 0 || w.row == from;
+    const int b = w.b;
+    w.row = n.row0 + n.last;
+    if (!begins) continue;                                // the block begins in rows before these
+    n.b = b, n.place = place & ~15;
+    return true;
+  }
+  return false;
+}
 
-      const int64_t block = kv8_block(a.pool, page, head, place & ((1 << a.pool.page_bits) - 1));
-      uint8_t* const scale = a.pool.scales + block * 2 + value;
-      uint8_t* const codes = a.pool.codes + (block * 2 + value) * (int64_t)(kBlockTokens * a.dim);
-      const uint32_t had = first > 0 ? *scale : 0u;
-      const uint16_t* const src = value ? a.v + head * a.v_head + lane * 8 : a.k + head * a.k_head + lane * 8;
-      const int64_t stride = value ? a.v_token : a.k_token;
-      Packed8 raw[TPL];
+// Keys or values (VALUE) of one head for one block, by LT * TG lanes: lane (t, l) has 8 channels of TPL places, so that the values' words, 4 places of a channel, are made
+// without another lane; all of a block's new tokens are there at once, and the largest magnitude takes one round of exchanges.  Only where the byte of scale
+// grows are the block's earlier tokens read at all.
+template <int LB>
+struct Unit {
+  static constexpr int LT = 1 << LB, TG = LT <= 16 ? 4 : 2, GROUP = LT * TG, TPL = 16 / TG, PAIRS = kWave / GROUP;
+  Packed8 raw[TPL];
+  int head;
+  bool there;
+};
+template <int LB, bool VALUE>
+__device__ inline void load_unit(const AppendArgs& a, Unit<LB>& u, const NewTokens& n, int lane64) {
+  const int lane = lane64 & (Unit<LB>::LT - 1), first_place = (lane64 >> LB) % Unit<LB>::TG * Unit<LB>::TPL;
+  const uint16_t* const src = VALUE ? a.v + u.head * a.v_head + lane * 8 : a.k + u.head * a.k_head + lane * 8;
+  const int64_t stride = VALUE ? a.v_token : a.k_token;
 #pragma unroll
-      for (int r = 0; r < TPL; ++r) {
-        const int p = first_place + r;
-        raw[r] = Packed8{0, 0, 0, 0};
-        if (there && mine && p >= first && p < last) raw[r] = *reinterpret_cast<const Packed8Any*>(src + (int64_t)(row0 + p) * stride);
+  for (int r = 0; r < Unit<LB>::TPL; ++r) {
+    const int p = first_place + r;
+    u.raw[r] = Packed8{0, 0, 0, 0};
+    if (u.there && lane * 8 < a.dim && p >= n.first && p < n.last) u.raw[r] = *reinterpret_cast<const Packed8Any*>(src + (int64_t)(n.row0 + p) * stride);
+  }
+}
+__device__ inline bool is_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu) < 0x7F800000u; }
+// turn_at(place): what turns the keys of that token.
+template <bool BF, int LB, bool VALUE, class TurnAt>
+__device__ inline void store_unit(const AppendArgs& a, const Unit<LB>& u, const NewTokens& n, int page, int lane64, TurnAt turn_at) {
+  constexpr int LT = Unit<LB>::LT, TPL = Unit<LB>::TPL, GROUP = Unit<LB>::GROUP;
+  const int lane = lane64 & (LT - 1), first_place = (lane64 >> LB) % Unit<LB>::TG * TPL;
+  const bool mine = lane * 8 < a.dim;
+  const int64_t block = kv8_block(a.pool, page, u.head, n.place & ((1 << a.pool.page_bits) - 1));
+  uint8_t* const scale = a.pool.scales + block * 2 + VALUE;
+  uint8_t* const codes = a.pool.codes + (block * 2 + VALUE) * (int64_t)(kBlockTokens * a.dim);
+  const uint32_t had = n.first > 0 ? *scale : 0u;
+  float y[TPL][8];
+#pragma unroll
+  for (int r = 0; r < TPL; ++r) {
+    if constexpr (VALUE) unpack8<BF>(u.raw[r], y[r]);
+    else finish<BF, LT>(a, u.raw[r], a.k_weight, turn_at(min(max(first_place + r, n.first), n.last - 1)), lane, y[r]);
+  }
+  if (n.first > 0 || n.last < 16) {
+#pragma unroll
+    for (int r = 0; r < TPL; ++r) {
+      const bool fresh = first_place + r >= n.first && first_place + r < n.last;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[r][e] = fresh ? y[r][e] : 0.f;
+    }
+  }
+  float most = 0.f;
+  bool odd = false;                                       // something is not a number, or infinite
+#pragma unroll
+  for (int r = 0; r < TPL; ++r) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      most = fmaxf(most, fmaxf(fabsf(y[r][e]), fabsf(y[r][e + 1])));
+      odd = odd || __builtin_isunordered(y[r][e], y[r][e + 1]);
+    }
+  }
+  odd = odd || most == INFINITY;
+  const bool any_odd = __any(odd);
+  if (any_odd) {
+    most = 0.f;
+#pragma unroll
+    for (int r = 0; r < TPL; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, is_finite(y[r][e]) ? fabsf(y[r][e]) : 0.f);
+  }
+  const uint32_t byte = max(scale_byte(most_over<GROUP>(__builtin_bit_cast(uint32_t, most))), had);
+  const bool grown = n.first > 0 && byte > had;
+  const float down = power_of(254u - min(byte, 254u));
+  if (u.there && (lane64 & (GROUP - 1)) == 0 && (n.first == 0 || grown)) *scale = (uint8_t)byte;
+  const int begin = grown ? 0 : n.first;                  // places that are written
+  if (!u.there || !mine) return;
+  uint32_t word[TPL][2];                                  // 8 codes of a place
+#pragma unroll
+  for (int r = 0; r < TPL; ++r) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float* const x = y[r] + 4 * h;
+      int both = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * down, x[1] * down, 0, false);
+      word[r][h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * down, x[3] * down, both, true);
+    }
+  }
+  if (any_odd || byte >= kMostScale) {                    // what is not finite, and what 448 does not reach
+#pragma unroll
+    for (int r = 0; r < TPL; ++r) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = is_finite(y[r][4 * h + e]) ? y[r][4 * h + e] * down : 0.f;
+        word[r][h] = codes_of(x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) word[r][h] |= is_finite(y[r][4 * h + e]) ? 0u : 0x7Fu << 8 * e;
       }
-      float y[TPL][8];
-      uint32_t most = 0;
-      bool odd = false;                                   // something is not finite
+    }
+  }
+  if (grown) {                                            // the tokens in front again
+    const float again = power_of(127u - min(byte - had, 127u));
 #pragma unroll
-      for (int r = 0; r < TPL; ++r) {
-        const int p = first_place + r;
-        if (value) {
-          unpack8<BF>(raw[r], y[r]);
-        } else {
-          const Turn t = turn_of(a, row0 + min(max(p, first), last - 1), lane);
-          finish<BF, LT>(a, raw[r], a.k_weight, t, lane, y[r]);
-        }
-        if (p < first || p >= last) continue;
+    for (int r = 0; r < TPL; ++r) {
+      const int p = first_place + r;
+      if (p >= n.first) continue;
+      uint32_t old[2] = {0, 0};
+      if (VALUE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t bits = __builtin_bit_cast(uint32_t, y[r][e]) & 0x7FFFFFFFu;
-          odd = odd || bits >= 0x7F800000u;
-          most = max(most, bits >= 0x7F800000u ? 0u : bits);
+        for (int e = 0; e < 8; ++e) old[e >> 2] |= (uint32_t)codes[((p >> 2) * a.dim + lane * 8 + e) * 4 + (p & 3)] << 8 * (e & 3);
+      } else {
+        const W2 w = *reinterpret_cast<const W2*>(codes + p * a.dim + lane * 8);
+        old[0] = w[0], old[1] = w[1];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float z[4];
+        numbers_of(old[h], z);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = (old[h] >> 8 * e & 0x7Fu) == 0x7Fu ? 0.f : z[e] * again;
+        uint32_t w = codes_of(z);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w |= (old[h] >> 8 * e & 0x7Fu) == 0x7Fu ? 0x7Fu << 8 * e : 0u;
+        word[r][h] = w;
+      }
+    }
+  }
+  if constexpr (!VALUE) {
+#pragma unroll
+    for (int r = 0; r < TPL; ++r) {
+      const int p = first_place + r;
+      if (p >= begin && p < n.last) *reinterpret_cast<W2*>(codes + p * a.dim + lane * 8) = W2{word[r][0], word[r][1]};
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < TPL / 4; ++q) {
+      const int p = first_place + 4 * q;
+      uint8_t* const quad = codes + ((p >> 2) * a.dim + lane * 8) * 4;
+      uint32_t out[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t rows4[4] = {word[4 * q][h], word[4 * q + 1][h], word[4 * q + 2][h], word[4 * q + 3][h]};
+        uint32_t cols[4];
+        turn_words(rows4, cols);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[4 * h + e] = cols[e];
+      }
+      if (p >= begin && p + 4 <= n.last) {
+        *reinterpret_cast<W4*>(quad) = W4{out[0], out[1], out[2], out[3]};
+        *reinterpret_cast<W4*>(quad + 16) = W4{out[4], out[5], out[6], out[7]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (p + i < begin || p + i >= n.last) continue;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) quad[e * 4 + i] = (uint8_t)(out[e] >> 8 * i);
         }
       }
-      const uint32_t byte = max(scale_byte(most_over<GROUP>(most)), had);
-      const bool grown = first > 0 && byte > had;
-      const float down = power_of(254u - min(byte, 254u)), again = power_of(127u - min(byte - had, 127u));
-      if (there && (lane64 & (GROUP - 1)) == 0 && (first == 0 || grown)) *scale = (uint8_t)byte;
-      const int begin = grown ? 0 : first;                // places that are written
-      if (!there || !mine) continue;
-      uint32_t word[TPL][2];                              // 8 codes of a place
-#pragma unroll
-      for (int r = 0; r < TPL; ++r) {
-        const int p = first_place + r;
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = y[r][e] * down;
-        word[r][0] = codes_of(x), word[r][1] = codes_of(x + 4);
-        if (odd) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if ((__builtin_bit_cast(uint32_t, y[r][e]) & 0x7FFFFFFFu) >= 0x7F800000u)
-              word[r][e >> 2] = (word[r][e >> 2] & ~(255u << 8 * (e & 3))) | 0x7Fu << 8 * (e & 3);
-          }
-        }
-        if (grown && p < first) {
-          uint32_t old[2];
-          if (value) {
-            old[0] = old[1] = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) old[e >> 2] |= (uint32_t)codes[((p >> 2) * a.dim + lane * 8 + e) * 4 + (p & 3)] << 8 * (e & 3);
-          } else {
-            const W2 w = *reinterpret_cast<const W2*>(codes + p * a.dim + lane * 8);
-            old[0] = w[0], old[1] = w[1];
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float z[4];
-            numbers_of(old[h], z);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] *= again;
-            uint32_t w = codes_of(z);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if ((old[h] >> 8 * e & 0x7Fu) == 0x7Fu) w = (w & ~(255u << 8 * e)) | 0x7Fu << 8 * e;
-            }
-            word[r][h] = w;
-          }
-        }
-        if (!value && p >= begin && p < last) *reinterpret_cast<W2*>(codes + p * a.dim + lane * 8) = W2{word[r][0], word[r][1]};
+    }
+  }
+}
+
+// Few tokens: a workgroup either turns queries of a token (groups of LT lanes take a head) or stores the block that begins in a row: each wavefront the keys or
+// the values of one head or, where a block takes fewer lanes, of several.
+template <bool BF, int LB>
+__global__ __launch_bounds__(kBlock) void append_kernel(const AppendArgs a) {
+  constexpr int LT = 1 << LB, GROUP = Unit<LB>::GROUP, PAIRS = Unit<LB>::PAIRS;
+  const int lane64 = threadIdx.x & 63, lane = lane64 & (LT - 1);
+  if ((int)blockIdx.x < a.q_groups) {
+    const int head = (int)blockIdx.x * (kBlock / LT) + (threadIdx.x >> LB);
+    const bool there = head < a.heads && lane * 8 < a.dim;
+    for (int64_t token = blockIdx.y; token < a.tokens; token += gridDim.y) {
+      Packed8 raw = {0, 0, 0, 0};
+      if (there) raw = *reinterpret_cast<const Packed8Any*>(a.q + token * a.q_token + head * a.q_head + lane * 8);
+      float y[8];
+      finish<BF, LT>(a, raw, a.q_weight, turn_of(a, token, lane), lane, y);
+      if (there) *reinterpret_cast<Packed8Any*>(a.out + token * a.out_token + head * a.out_head + lane * 8) = pack8<BF>(y);
+    }
+    return;
+  }
+  const int rest = ((int)blockIdx.x - a.q_groups) * (kBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // keys' heads, then values'
+  if (rest >= 2 * a.groups) return;
+  const int head = (rest >= a.groups ? rest - a.groups : rest) * PAIRS + lane64 / GROUP;
+  Unit<LB> u;
+  u.there = head < a.pool.heads;
+  u.head = u.there ? head : 0;
+  auto store = [&](auto value) {
+    constexpr bool VALUE = decltype(value)::value;
+    for (int64_t chunk = blockIdx.y; chunk < a.tokens; chunk += gridDim.y) {
+      Walk w = walk_of(a, chunk, lane64);
+      NewTokens n;
+      while (next_block(a, w, n)) {
+        load_unit<LB, VALUE>(a, u, n, lane64);            // under way before the page is known
+        const int page = page_of(a, n);
+        if (page >= 0) store_unit<BF, LB, VALUE>(a, u, n, page, lane64, [&](int place) { return turn_of(a, n.row0 + place, lane); });
       }
-      if (!value) continue;
-#pragma unroll
-      for (int u = 0; u < TPL / 4; ++u) {
-        const int p = first_place + 4 * u;
-        uint8_t* const quad = codes + ((p >> 2) * a.dim + lane * 8) * 4;
-        uint32_t out[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t rows4[4] = {word[4 * u][h], word[4 * u + 1][h], word[4 * u + 2][h], word[4 * u + 3][h]};
-          uint32_t cols[4];
-          turn_words(rows4, cols);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[4 * h + e] = cols[e];
-        }
-        if (p >= begin && p + 4 <= last) {
-          *reinterpret_cast<W4*>(quad) = W4{out[0], out[1], out[2], out[3]};
-          *reinterpret_cast<W4*>(quad + 16) = W4{out[4], out[5], out[6], out[7]};
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (p + i < begin || p + i >= last) continue;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) quad[e * 4 + i] = (uint8_t)(out[e] >> 8 * i);
-          }
-        }
+    }
+  };
+  if (rest >= a.groups) store(std::integral_constant<bool, true>{});
+  else store(std::integral_constant<bool, false>{});
+}
+
+// Many tokens, keys and values alone: a workgroup takes the blocks that begin in 16 rows, for the keys or the values of 4 times as many heads as a wavefront has
+// at once.  What turns the keys is brought into LDS once for all of them.
+template <bool BF, int LB>
+__global__ __launch_bounds__(kBlock, LB <= 4 ? 3 : 2) void blocks_kernel(const AppendArgs a) {
+  constexpr int LT = 1 << LB, GROUP = Unit<LB>::GROUP, PAIRS = Unit<LB>::PAIRS;
+  __shared__ __align__(16) float table[16 * 256];         // [place][cosines, sines]
+  __shared__ int placed[16];
+  const int lane64 = threadIdx.x & 63, lane = lane64 & (LT - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rest = blockIdx.x, head = ((rest >= a.groups ? rest - a.groups : rest) * 4 + wave) * PAIRS + lane64 / GROUP;
+  const int64_t chunks = (a.tokens + 15) >> 4;
+  Unit<LB> u;
+  u.there = head < a.pool.heads;
+  u.head = u.there ? head : 0;
+  NewTokens n;
+  if (rest >= a.groups) {
+    for (int64_t chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
+      Walk w = walk_of(a, chunk, lane64);
+      while (next_block(a, w, n)) {
+        load_unit<LB, true>(a, u, n, lane64);
+        const int page = page_of(a, n);
+        if (page >= 0) store_unit<BF, LB, true>(a, u, n, page, lane64, [&](int) { return Turn{}; });
       }
+    }
+    return;
+  }
+  const int quads = a.rot / 4;
+  for (int64_t chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
+    Walk w = walk_of(a, chunk, lane64);
+    while (next_block(a, w, n)) {
+      load_unit<LB, false>(a, u, n, lane64);
+      const int page = page_of(a, n);
+      if (a.rot > 0) {
+        __syncthreads();                                  // the block before has been turned
+        // 16 threads bring a token's row
+        const int place = threadIdx.x >> 4;
+        if (place >= n.first && place < n.last) {
+          const int64_t at = a.positions[n.row0 + place];
+          const bool fine = at >= 0 && at < a.table_rows;
+          if (fine)
+            for (int i = threadIdx.x & 15; i < quads; i += 16) reinterpret_cast<V4*>(table)[place * quads + i] = *reinterpret_cast<const V4*>(a.table + at * a.rot + i * 4);
+          if ((threadIdx.x & 15) == 0) placed[place] = fine;
+        }
+        __syncthreads();
+      }
+      if (page >= 0)
+        store_unit<BF, LB, false>(a, u, n, page, lane64, [&](int place) { return turn_by(a, table + place * a.rot, a.rot == 0 || placed[place], lane); });
     }
   }
 }
@@ -401,24 +522,27 @@ int pool_of(const macko_kv8_cache_t* c, bool data, Kv8Pool* p) {
   return MACKO_OK;
 }
 
-// Rows that a wavefront looks for blocks in: 16 where long sequences are likely (one block begins in them) and the launch is large, else 1.
+// Calls of many tokens of sequences: keys and values by a kernel that goes by 16 rows, queries by macko_rotate's.  From this many wavefronts of keys and values on, by row.
 constexpr int64_t kManyWaves = 16384;
 
 template <bool BF, int LB>
 int launch_append(AppendArgs& a, hipStream_t stream) {
-  constexpr int LT = 1 << LB, PAIRS = kWave / (LT * (LT <= 16 ? 4 : 2));
-  constexpr int kBundle = 4;
-  const int64_t cus = device_cu_count();
-  const bool bundle = (a.tokens * a.heads) / (kWave / LT) >= cus * 32;
-  a.bundles = a.heads == 0 ? 1 : bundle ? (a.heads + kBundle - 1) / kBundle : a.heads;
-  a.q_items = a.heads == 0 ? 0 : a.tokens * a.bundles;
-  a.q_waves = (a.q_items + kWave / LT - 1) / (kWave / LT);
-  a.pair_waves = (2 * a.pool.heads + PAIRS - 1) / PAIRS;
-  a.rows = a.start && a.tokens * a.pair_waves >= kManyWaves ? 16 : 1;
-  a.waves = a.q_waves + (a.tokens + a.rows - 1) / a.rows * a.pair_waves;
-  const dim3 grid((unsigned)std::min(kMostBlocks, (a.waves + kBlock / kWave - 1) / (kBlock / kWave))), block(kBlock);
-  if (bundle) hipLaunchKernelGGL((append_kernel<BF, LB, kBundle>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((append_kernel<BF, LB, 1>), grid, block, 0, stream, a);
+  constexpr int LT = 1 << LB, PAIRS = Unit<LB>::PAIRS;
+  a.groups = (a.pool.heads + PAIRS - 1) / PAIRS;
+  const dim3 block(kBlock);
+  if (a.start && a.tokens * 2 * a.groups >= kManyWaves) {
+    a.rows = 16;
+    a.groups = (a.groups + 3) / 4;
+    hipLaunchKernelGGL((blocks_kernel<BF, LB>), dim3((unsigned)(2 * a.groups), (unsigned)std::min<int64_t>(kMostGrid, (a.tokens + 15) / 16)), block, 0, stream, a);
+    MACKO_HIP_TRY(hipGetLastError());
+    if (a.heads == 0) return MACKO_OK;
+    const macko_rotation_t r{a.positions, a.table, a.table_rows, a.rot, a.interleaved, a.eps};
+    return macko_rotate(a.tokens, a.heads, a.dim, BF ? MACKO_BF16 : MACKO_FP16, a.q, a.q_token, a.q_head, &r, a.q_weight, a.out, a.out_token, a.out_head, stream);
+  }
+  a.rows = 1;
+  a.q_groups = (a.heads + kBlock / LT - 1) / (kBlock / LT);
+  const dim3 grid((unsigned)(a.q_groups + (2 * a.groups + kBlock / kWave - 1) / (kBlock / kWave)), (unsigned)std::min<int64_t>(kMostGrid, a.tokens));
+  hipLaunchKernelGGL((append_kernel<BF, LB>), grid, block, 0, stream, a);
   MACKO_HIP_TRY(hipGetLastError());
   return MACKO_OK;
 }
