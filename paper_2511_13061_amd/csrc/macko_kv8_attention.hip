@@ -336,8 +336,41 @@ __global__ __launch_bounds__(64 * kWaves, waves_wanted(NG, RT)) void attention8_
 // Two tiles of rows share the decoded values where there are more rows than one has.
 int row_tiles(const KvAttention& a) { return (int64_t)a.most_queries * a.shared > 16 && a.pool.dim <= 128 ? 2 : 1; }
 
-// Rows of a sequence up to which the kernel for few rows takes a call.
+// Rows of a sequence up to which the kernel for few rows takes a call; beyond, the estimates decide.
 constexpr int kFewRows = 64;
+
+struct Dealt {
+  int64_t splits;
+  double time;
+};
+// How many parts the tokens of a sequence are dealt out to: the number with the shortest estimate, in microseconds.  A workgroup goes on by 128 tokens in the
+// time that it takes alone, or that the workgroups of a compute unit take for one each where that is longer: from memory (5.6 TB/s, once for all rows of a sequence)
+// or on the vector units and matrix cores.  Workgroups take turns where more of them come than fit.  Joining costs a launch and the sums' way through memory.
+// Constants from 1828 timings, of 1 to 64 sequences of 1024 to 131072 tokens, 1 to 1024 rows on a key/value head of 64, 128 and 256 channels, with 1 to 128
+// parts, by both kernels where there are more than 16 rows; what it chooses took 0.7 % longer than the best of these in the mean, 20 % at worst.
+Dealt deal(const KvAttention& a, bool many, int64_t row_blocks, int64_t units) {
+  static constexpr int kTry[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
+  static_assert(kMostSplits == 256, "the last one tried");
+  const int64_t others = (int64_t)a.batch * a.pool.heads * row_blocks;
+  const double cus = device_cu_count(), rows = (double)a.tokens * a.heads, width = a.pool.dim / 128.0;
+  const bool two = row_tiles(a) == 2;
+  const double begin = many ? 1.9 : 2.8, alone = many ? 4.3 * (0.4 + 0.6 * width) : (two ? 1.3 : 1.1) * (0.5 + 0.5 * width);
+  const double memory = 128.0 * a.pool.dim * 2 * cus / 5.6e6 / (double)row_blocks, work = (many ? 0.97 : two ? 0.96 : 1.03) * (0.3 + 0.7 * width);
+  const double share = many ? work : std::max(memory, work), room = many ? (a.pool.dim <= 128 ? 2 : 1) : a.pool.dim <= 64 ? 3 : a.pool.dim <= 128 ? 2 : 1;
+  auto time = [&](int64_t splits) {
+    const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);
+    const double turns = groups <= 4.0 * room ? std::ceil(groups / room) : groups / room + 0.5;
+    return turns * (begin + steps * std::max(alone, busy * share)) + (splits > 1 ? 3.7 + rows * (double)splits * (a.pool.dim + 2) * 8.0 / 3.7e6 : 0.0);
+  };
+  Dealt best{1, time(1)};
+  if (!may_join(a)) return best;
+  for (const int splits : kTry) {
+    if (splits > units) break;
+    const double t = time(splits);
+    if (t < best.time) best = Dealt{splits, t};
+  }
+  return best;
+}
 
 Grid grid_of(const KvAttention& a) {
   Grid g{};
@@ -345,12 +378,18 @@ Grid grid_of(const KvAttention& a) {
   g.shared_inverse = a.shared == 1 ? 0u : (uint32_t)(((uint64_t{1} << 32) + a.shared - 1) / a.shared);
   const int64_t unit = g.unit, most_rows = (int64_t)a.most_queries * a.shared;
   const int64_t longest = std::max<int64_t>(1, std::min({a.longest, (int64_t)kMostTokens, a.window ? (int64_t)a.window + a.most_queries + 15 : a.longest}));
-  const bool many = tuning().attention_kernel ? tuning().attention_kernel == 2 : most_rows > kFewRows;
-  g.rows = many ? 32 * kWaves : 16 * row_tiles(a);
-  const int64_t row_blocks = (most_rows + g.rows - 1) / g.rows, others = (int64_t)a.batch * a.pool.heads * row_blocks, units = (longest + unit - 1) / unit;
-  int64_t splits = std::max<int64_t>(1, std::min({(int64_t)device_cu_count() * 2 / others, units / 4, (int64_t)kMostSplits}));
-  if (tuning().attention_parts > 0) splits = std::min({tuning().attention_parts, units, (int64_t)kMostSplits});
-  if (!may_join(a)) splits = 1;
+  auto block_rows = [&](bool many) { return many ? 32 * kWaves : 16 * row_tiles(a); };
+  auto dealt = [&](bool many) { return deal(a, many, std::max<int64_t>(1, (most_rows + block_rows(many) - 1) / block_rows(many)), (longest + unit - 1) / unit); };
+  const Tuning& knobs = tuning();
+  bool many = knobs.attention_kernel == 2;
+  Dealt best = dealt(many);
+  if (knobs.attention_kernel == 0 && most_rows > kFewRows) {
+    const Dealt other = dealt(true);
+    if (other.time < best.time) best = other, many = true;
+  }
+  if (knobs.attention_parts > 0 && may_join(a)) best.splits = std::min({knobs.attention_parts, (longest + unit - 1) / unit, (int64_t)kMostSplits});
+  g.rows = block_rows(many);
+  const int64_t splits = best.splits, row_blocks = (most_rows + g.rows - 1) / g.rows, others = (int64_t)a.batch * a.pool.heads * row_blocks;
   g.chunk = (longest + splits * unit - 1) / (splits * unit) * unit;
   g.splits = (int32_t)((longest + g.chunk - 1) / g.chunk);
   g.row_blocks = (int32_t)std::min(row_blocks, kMostGrid / g.splits);      // of a launch: a workgroup goes on to others
