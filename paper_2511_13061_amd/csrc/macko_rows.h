@@ -59,6 +59,9 @@ __device__ inline U2 read_turned(const uint8_t* at) {
   return __builtin_bit_cast(U2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(__attribute__((address_space(3))) void*)at));
 }
 
+// NaN where one of them is.
+__device__ inline float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
 // The sum of a pair's two numbers and x.
 template <bool HALF>
 __device__ inline float add_pair(int pair, float x) {
@@ -341,7 +344,8 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   float base = 0.f, limit = -INFINITY;                    // what scores are lifted by, and how large they may then be; nothing seen yet: 0 and -infinity
   float sum = 0.f, rest = 0.f, full = 0.f;                // of the weights as they are multiplied, what its roundings left out; of the weights before they are rounded
   V16f out[NG];
-  const int want_sums = __builtin_amdgcn_readfirstlane(a.sums != nullptr);
+  const int want_sums_now = __builtin_amdgcn_readfirstlane(a.sums != nullptr);
+  constexpr bool kSumsApart = !PAGED && NG <= 2;          // loops of their own for calls with sums: else the weights are made twice there, for want of registers
   auto begin_rows = [&] {
     base = 0.f, limit = -INFINITY, sum = rest = full = 0.f;
 #pragma unroll
@@ -350,16 +354,20 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   // what scores of tokens 16 e on are multiplied with
   auto unit_of = [&](int number, int e) { return PAGED && !BF ? lds_unit[(number & 3) * 4 + e] : unit; };
   auto hide = [&](V16f& x, int at) {
+    // the lane's tokens are at + 4 h + (0 .. 3), + 8 and so on: it sees those from `from` to before `to`, a bit each
+    const int behind = max(place + 1 - at - 4 * (later(threadIdx.x) >> 5 & 1), 0), from = min(max(behind - (int)reach, 0), 32), to = min(behind, 32);
+    const uint32_t seen = (uint32_t)(((uint64_t{1} << to) - 1) & ~((uint64_t{1} << from) - 1));
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int token = at + (i & 3) + 8 * (i >> 2) + 4 * h;
-      if ((uint32_t)(place - token) >= reach) x[i] = -INFINITY;
+      const uint32_t keep = (uint32_t)((int32_t)(seen << (31 - ((i & 3) + 8 * (i >> 2)))) >> 31);
+      const float score = x[i];                           // a cast of an element's bits takes the first one's
+      x[i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, score) & keep) | (0xFF800000u & ~keep));
     }
   };
   auto largest_of = [&](const V16f& x, int half) {
-    float most = fmaxf(x[8 * half], x[8 * half + 1]);
+    float most = larger(x[8 * half], x[8 * half + 1]);
 #pragma unroll
-    for (int i = 2; i < 8; i += 2) most = fmaxf(most, fmaxf(x[8 * half + i], x[8 * half + i + 1]));
+    for (int i = 2; i < 8; i += 2) most = larger(larger(most, x[8 * half + i]), x[8 * half + i + 1]);
     return most;
   };
   // `most`: the largest lifted score of the step
@@ -382,7 +390,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   };
 
   // A step's products with the scores of the one behind it: while the matrix cores are at those, the vector units weigh this one's.
-  auto step = [&](int at, int number, int buffer, V16f (&x)[PARTS], V16f (&next)[PARTS], float (&top)[2 * PARTS], auto between) {
+  auto step = [&](int at, int number, int buffer, V16f (&x)[PARTS], V16f (&next)[PARTS], float (&top)[2 * PARTS], auto want_sums, auto bring_values) {
     constexpr float kTop = HALF ? 10.f : 0.f, kMost = kTop + (HALF ? 5.f : kLift);
     if (at < all_lo || at + STEP > all_hi) {
       asm volatile("");                                   // a branch, not selections that every step would make
@@ -398,16 +406,18 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       most = fmaxf(most, __builtin_fmaf(top[e], units[e], base));
     }
     if (__any(most > limit)) lift(most, kTop, kMost);
-    if (want_sums) {
-      float more = 0.f, same = base;
-      asm volatile("" : "+v"(same));                      // weights of their own: those below would be made here, not beside the products
+    if constexpr (!kSumsApart) {
+      if (want_sums_now) {
+        float more = 0.f, same = base;
+        asm volatile("" : "+v"(same));                    // weights of their own: those below would be made here, not beside the products
 #pragma unroll
-      for (int i = 0; i < 16 * PARTS; ++i) more += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i / 16][i % 16], units[i / 8], same));
-      full += more;
+        for (int i = 0; i < 16 * PARTS; ++i) more += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i / 16][i % 16], units[i / 8], same));
+        full += more;
+      }
     }
     constexpr int kKeyFlight = PAGED ? 2 : 3;             // steps of keys' operands on their way; what the registers hold
     V4i p[2 * PARTS], key[kKeyFlight][PARTS];
-    float more = 0.f;
+    float more = 0.f, exact = 0.f;
 #pragma unroll
     for (int part = 0; part < PARTS; ++part) {
       next[part] = V16f{};
@@ -431,9 +441,11 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
         asm volatile("" : "+v"(both));                    // here, not where it is used
         p[i / 8][i % 8 / 2] = both;
         more = add_pair<HALF>(both, more);
+        if constexpr (decltype(want_sums)::value) exact += w0 + w1;
       }
     }
-    between();
+    if constexpr (decltype(want_sums)::value) full += exact;
+    bring_values();
     constexpr int kFlight = 4, kAll = NG * 2 * PARTS;     // values' operands on their way
     V4i value[kFlight];
 #pragma unroll
@@ -448,7 +460,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       for (int pair = k * 8 * PARTS / kAll; pair < (k + 1) * 8 * PARTS / kAll; ++pair) {
         const int i = 2 * pair;
         const float x0 = next[i / 16][i % 16], x1 = next[i / 16][i % 16 + 1];
-        top[i / 8] = i % 8 == 0 ? fmaxf(x0, x1) : fmaxf(top[i / 8], fmaxf(x0, x1));
+        top[i / 8] = i % 8 == 0 ? larger(x0, x1) : larger(larger(top[i / 8], x0), x1);
       }
     }
     add_sum(more);
@@ -541,10 +553,10 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       for (int i = 0; i < STEP / 16; ++i) byte = max(byte, lds_word[i]);
       first_byte = __builtin_amdgcn_readfirstlane((int)byte);
     }
-    store_keys(0);
-    store_values(begin, 0, No{});
     int slot = 1;                                         // of the next keys' pages
     int64_t value_block = 0;
+    store_keys(0);
+    store_values(begin, 0, No{});
     if (begin + STEP < end) {
       load_keys(begin + STEP, slot);
       value_block = key_block;
@@ -562,7 +574,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     }
     __syncthreads();
     int number = 0;
-    auto turn = [&](int at, int buffer, V16f (&x)[PARTS], V16f (&next)[PARTS]) {
+    auto turn = [&](int at, int buffer, V16f (&x)[PARTS], V16f (&next)[PARTS], auto want_sums) {
       // keys of the step behind the next; what is looked up for them serves the values a step later
       const int64_t block = !BOTH && PAGED && brings_values && at + STEP < end ? block_of(at + STEP, slot) : value_block;
       ++slot;
@@ -574,7 +586,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
         load_keys(at + 2 * STEP, slot);
         value_block = key_block;
       }
-      step(at, number, buffer, x, next, top, [&] {
+      step(at, number, buffer, x, next, top, want_sums, [&] {
         if (at + STEP < end) load_values(at + STEP, block);
       });
       if (at + 2 * STEP < end) store_keys(number + 2);
@@ -582,11 +594,15 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       ++number;
       __syncthreads();
     };
-    for (int at = begin; at < end; at += 2 * STEP) {
-      turn(at, 0, scores[0], scores[1]);
-      if (at + STEP >= end) break;
-      turn(at + STEP, 1, scores[1], scores[0]);
-    }
+    auto go = [&](auto want_sums) {
+      for (int at = begin; at < end; at += 2 * STEP) {
+        turn(at, 0, scores[0], scores[1], want_sums);
+        if (at + STEP >= end) break;
+        turn(at + STEP, 1, scores[1], scores[0], want_sums);
+      }
+    };
+    if (kSumsApart && a.sums) go(std::integral_constant<bool, kSumsApart>{});
+    else go(No{});
     float all = 0.f;
 #pragma unroll
     for (int c = 0; c < NG; ++c)
