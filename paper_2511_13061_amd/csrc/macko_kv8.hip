@@ -133,8 +133,8 @@ __device__ inline int page_of(const AppendArgs& a, const NewTokens& n) {
   const int index = n.place >> a.pool.page_bits, page = index < a.table_width ? constant(a.tables + n.b * a.table_stride + index) : -1;
   return page >= 0 && page < a.pool.pages ? page : -1;
 }
-__device__ inline Walk walk_of(const AppendArgs& a, int64_t chunk, int lane64) {
-  Walk w{(int)(chunk * a.rows), (int)min((chunk + 1) * a.rows, a.tokens), 0};
+__device__ inline Walk walk_of(const AppendArgs& a, int chunk, int lane64) {
+  Walk w{chunk * a.rows, min((chunk + 1) * a.rows, (int)a.tokens), 0};
   w.b = a.start ? sequence_at(a.start, a.batch, w.row, lane64) : w.row;
   if (w.b < 0) w.b = 0, w.row = min(max(a.start[0], 0), w.end);
   return w;
@@ -199,6 +199,7 @@ __device__ inline void store_unit(const AppendArgs& a, const Unit<LB>& u, const 
   float y[TPL][8];
 #pragma unroll
   for (int r = 0; r < TPL; ++r) {
+    __builtin_amdgcn_sched_barrier(0);                    // one place's cosines and sines at a time, and so below: what more hold of registers costs wavefronts
     if constexpr (VALUE) unpack8<BF>(u.raw[r], y[r]);
     else finish<BF, LT>(a, u.raw[r], a.k_weight, turn_at(min(max(first_place + r, n.first), n.last - 1)), lane, y[r]);
   }
@@ -210,19 +211,14 @@ __device__ inline void store_unit(const AppendArgs& a, const Unit<LB>& u, const 
       for (int e = 0; e < 8; ++e) y[r][e] = fresh ? y[r][e] : 0.f;
     }
   }
-  float most = 0.f;
-  bool odd = false;                                       // something is not a number, or infinite
+  float most = 0.f;                                       // NaN where something is
 #pragma unroll
-  for (int r = 0; r < TPL; ++r) {
+  for (int r = 0; r < TPL; ++r)
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      most = fmaxf(most, fmaxf(fabsf(y[r][e]), fabsf(y[r][e + 1])));
-      odd = odd || __builtin_isunordered(y[r][e], y[r][e + 1]);
-    }
-  }
-  odd = odd || most == INFINITY;
-  const bool any_odd = __any(odd);
+    for (int e = 0; e < 8; ++e) most = __builtin_elementwise_maximum(most, fabsf(y[r][e]));
+  const bool any_odd = __any(!(most < INFINITY));
   if (any_odd) {
+    asm volatile("");                                     // a branch, not selections that every block would make; so below
     most = 0.f;
 #pragma unroll
     for (int r = 0; r < TPL; ++r)
@@ -245,12 +241,14 @@ __device__ inline void store_unit(const AppendArgs& a, const Unit<LB>& u, const 
       word[r][h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * down, x[3] * down, both, true);
     }
   }
-  if (any_odd || byte >= kMostScale) {                    // what is not finite, and what 448 does not reach
+  if (any_odd || __any(byte >= kMostScale)) {             // what is not finite, and what 448 does not reach
+    asm volatile("");
 #pragma unroll
     for (int r = 0; r < TPL; ++r) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float x[4];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = is_finite(y[r][4 * h + e]) ? y[r][4 * h + e] * down : 0.f;
         word[r][h] = codes_of(x);
@@ -264,6 +262,7 @@ __device__ inline void store_unit(const AppendArgs& a, const Unit<LB>& u, const 
 #pragma unroll
     for (int r = 0; r < TPL; ++r) {
       const int p = first_place + r;
+      __builtin_amdgcn_sched_barrier(0);
       if (p >= n.first) continue;
       uint32_t old[2] = {0, 0};
       if (VALUE) {
@@ -347,7 +346,7 @@ __global__ __launch_bounds__(kBlock) void append_kernel(const AppendArgs a) {
   u.head = u.there ? head : 0;
   auto store = [&](auto value) {
     constexpr bool VALUE = decltype(value)::value;
-    for (int64_t chunk = blockIdx.y; chunk < a.tokens; chunk += gridDim.y) {
+    for (int chunk = blockIdx.y; chunk < (int)a.tokens; chunk += gridDim.y) {
       Walk w = walk_of(a, chunk, lane64);
       NewTokens n;
       while (next_block(a, w, n)) {
@@ -364,19 +363,19 @@ __global__ __launch_bounds__(kBlock) void append_kernel(const AppendArgs a) {
 // Many tokens, keys and values alone: a workgroup takes the blocks that begin in 16 rows, for the keys or the values of 4 times as many heads as a wavefront has
 // at once.  What turns the keys is brought into LDS once for all of them.
 template <bool BF, int LB>
-__global__ __launch_bounds__(kBlock, LB <= 4 ? 3 : 2) void blocks_kernel(const AppendArgs a) {
+__global__ __launch_bounds__(kBlock, LB <= 4 ? 4 : 2) void blocks_kernel(const AppendArgs a) {
   constexpr int LT = 1 << LB, GROUP = Unit<LB>::GROUP, PAIRS = Unit<LB>::PAIRS;
   __shared__ __align__(16) float table[16 * 256];         // [place][cosines, sines]
   __shared__ int placed[16];
   const int lane64 = threadIdx.x & 63, lane = lane64 & (LT - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rest = blockIdx.x, head = ((rest >= a.groups ? rest - a.groups : rest) * 4 + wave) * PAIRS + lane64 / GROUP;
-  const int64_t chunks = (a.tokens + 15) >> 4;
+  const int chunks = (int)((a.tokens + 15) >> 4);
   Unit<LB> u;
   u.there = head < a.pool.heads;
   u.head = u.there ? head : 0;
   NewTokens n;
   if (rest >= a.groups) {
-    for (int64_t chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
+    for (int chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
       Walk w = walk_of(a, chunk, lane64);
       while (next_block(a, w, n)) {
         load_unit<LB, true>(a, u, n, lane64);
@@ -387,7 +386,7 @@ __global__ __launch_bounds__(kBlock, LB <= 4 ? 3 : 2) void blocks_kernel(const A
     return;
   }
   const int quads = a.rot / 4;
-  for (int64_t chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
+  for (int chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
     Walk w = walk_of(a, chunk, lane64);
     while (next_block(a, w, n)) {
       load_unit<LB, false>(a, u, n, lane64);
