@@ -13,14 +13,16 @@ int launch_waves(LaunchRows& l, int64_t blocks, hipStream_t stream) {
   return launch_rows<NG, BF, false, WAVES>(l, dim3((unsigned)(blocks * l.a.pool.heads)), stream);
 }
 
-// Heads of 96 and 128 channels: eight wavefronts, which bring a step's keys and values for 256 rows, where those blocks fill the device twice, else four (32 heads on 8 of 128 channels,
-// bf16: 4096 tokens 160 us, 180 with four; 1024 tokens 33 us with four, 40 with eight).
+// Heads of 96 and 128 channels: eight wavefronts, which bring a step's keys and values for 256 rows, where those blocks fill the device twice and rows see some 512 tokens
+// in the mean, else four, which waste less at both ends of what a block sees.  128 channels, 32 heads on 8: bf16, one sequence of 4096 tokens 160 us, 180 with four;
+// of 1024 tokens 40 us, 33 with four; fp16, 12800 tokens in sequences of 2048 276 us, 293 with four; of 1024 178 and 180; of 512 140 and 128; of 64 101 and 79.
 template <int NG, bool BF>
 int launch_type(LaunchRows& l, hipStream_t stream) {
   const int64_t rows = l.a.tokens * l.a.shared;
   if constexpr (NG == 3 || NG == 4) {
     const int64_t blocks = (rows + 255) / 256;
-    if (blocks * l.a.pool.heads >= 2 * (int64_t)device_cu_count()) return launch_waves<NG, BF, 8>(l, blocks, stream);
+    const int64_t seen = l.a.window ? std::min<int64_t>(l.a.window, l.a.longest / 2) : l.a.longest / 2;
+    if (seen >= 512 && blocks * l.a.pool.heads >= 2 * (int64_t)device_cu_count()) return launch_waves<NG, BF, 8>(l, blocks, stream);
   }
   return launch_waves<NG, BF, 4>(l, (rows + 127) / 128, stream);
 }
@@ -55,6 +57,7 @@ int macko_prompt_attention(const macko_prompt_args_t* g, void* stream) {
   a.start = g->start_dev, a.batch = g->batch;
   a.heads = g->heads, a.shared = g->heads / g->kv_heads, a.window = g->window;
   a.scale = g->scale, a.tokens = g->tokens, a.type = g->type;
+  a.longest = g->start_dev ? std::min(g->longest, g->tokens) : g->tokens;
   l.k = static_cast<const uint16_t*>(g->k_dev), l.k_token = g->k_token, l.k_head = g->k_head;
   l.v = static_cast<const uint16_t*>(g->v_dev), l.v_token = g->v_token, l.v_head = g->v_head;
   l.g.splits = 1;
