@@ -88,6 +88,9 @@ APPENDS = [
     (6, 3, 192, 128, 64, True, False, [[19, 120], [100, 20]]),
     (2, 1, 224, 16, 224, False, False, [[18], [18]]),
     (8, 8, 256, 16, 128, True, True, [[40, 2, 9], [8, 14, 1]]),
+    # calls that go by 16 rows
+    (4, 8, 128, 32, 128, True, False, [[700, 1, 0, 400], [9, 600, 1, 500]]), (2, 16, 64, 16, 32, False, True, [[5, 1100, 30], [900, 17, 250]]),
+    (0, 40, 32, 64, 0, False, False, [[430, 440]]), (3, 6, 256, 16, 256, False, False, [[1400, 3], [16, 1390]]), (2, 8, 96, 128, 96, True, True, [[1] * 30 + [1100], [3] * 30 + [1000]]),
 ]
 
 
@@ -217,6 +220,51 @@ def test_append_of_what_has_no_place():
     assert cache.append(None, k[:0].cuda(), v[:0].cuda(), None, ints(tables[:0]), ints([])) is None
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,kv_heads", [(128, 8), (32, 32), (256, 6)])
+def test_append_of_many_sequences_is_that_of_each(dim, kv_heads, dtype):
+    """One call of many tokens against a call for every sequence: the same bytes in the pool.  Among them rows of no sequence in front and behind, more rows than
+    tokens, missing pages, tables that are too short, positions outside the table, blocks whose scale grows, values that are not finite."""
+    g = rng(dim)
+    page, heads, batch, rot = 32, 3, 90, 32
+    one, two = (pool(rng(5), 400, page, kv_heads, dim) for _ in range(2))
+    fresh = torch.randint(0, 40, (batch,), generator=g).tolist()
+    fresh[3], fresh[40], fresh[41] = 0, 150, 1
+    while sum(fresh) % 16 != 5:
+        fresh[7] += 1
+    past = [int(torch.randint(0, 70, (1,), generator=g)) for _ in fresh]
+    past[9] = -5                                                       # five rows have no place
+    lengths = np.array([p + n for p, n in zip(past, fresh)])
+    lengths[20] = -3
+    start = np.concatenate([[6], 6 + np.cumsum(fresh)])
+    tokens = int(start[-1]) + 9
+    assert tokens * 2 * kv_heads >= 16384                              # a wavefront has up to four heads of 32 channels, two of 64
+    if dim == 32:
+        tokens = 4 * tokens
+    tables = np.stack([np.arange(b, 400, batch)[:4] for b in range(batch)])
+    tables = np.concatenate([tables, tables[:, :1] + 3000], 1)         # 128 to 159: no page
+    tables[12, 0] = -1
+    x = [normal(g, tokens, h, dim, dtype=dtype, scale=2.0) for h in (heads, kv_heads, kv_heads)]
+    for t in x[1:]:
+        t *= torch.exp2(torch.randint(-5, 6, (tokens, 1, 1), generator=g)).to(dtype)
+        t[100, 0, 3], t[101, -1, 5], t[150, 1] = float("nan"), float("inf"), 0.0
+    at = torch.randint(0, 300, (tokens,), generator=g).numpy()
+    at[50], at[200] = 300, -2
+    tab, w = M.rope_table(300, rot), normal(g, dim, dtype=dtype).cuda()
+    q, k, v = (t.cuda() for t in x)
+    more = dict(table=tab, q_weight=w, k_weight=w, eps=1e-6)
+    got = one.append(q, k, v, ints(at), ints(tables), ints(lengths), start=ints(start), **more)
+    for b in range(batch):
+        lo, hi = start[b], start[b + 1]
+        if hi > lo:
+            want = two.append(q[lo:hi], k[lo:hi], v[lo:hi], ints(at[lo:hi]), ints(tables[b:b + 1]), ints(lengths[b:b + 1]), start=ints([0, hi - lo]), **more)
+            # 32 bits in both, in another order in the norm's sum perhaps: a unit in the last place
+            a, c = got[lo:hi].float().cpu(), want.float().cpu()
+            assert torch.equal(a.isnan(), c.isnan()) and ((a - c).abs() <= c.abs() * torch.finfo(dtype).eps + 1e-6).masked_fill(c.isnan(), True).all()
+    assert torch.equal(one.data, two.data) and torch.equal(one.scales, two.scales)
+    assert torch.isnan(got[[50, 200]]).all() and not torch.isnan(got[:6]).any()
+
+
 def test_offsets_beyond_32_bits():
     """Pages on both sides of 2^31 and 2^32 bytes of a pool, through all three calls."""
     page, heads, dim = 64, 8, 128
@@ -294,6 +342,51 @@ def test_attention(case, dtype):
         if more:
             more["most_queries"], weight = most, 2.0 ** -15 + 2.0 ** -11
         check_attention(cache.attend(q.cuda(), ints(tables), ints(lengths), window=window, longest=longest, **more), None, *want, dtype, weight)
+
+
+@pytest.fixture
+def knobs():
+    yield M.set_tuning
+    M.set_tuning("attention_kernel", 0)
+    M.set_tuning("attention_parts", 0)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 7, 256])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("case", [3, 11, 13, 15, 17, 19, 20, 22, 23, 24, 25, 26])
+def test_attention_by_either_kernel_in_parts(case, kernel, parts, knobs):
+    """Both kernels over rows that the other one would be taken for, with more parts than a sequence has tokens for among them."""
+    for dtype in TYPES:
+        cache, q, tables, lengths, n, window, want, more = attention_case(case, dtype)
+        knobs("attention_kernel", kernel)
+        knobs("attention_parts", parts)
+        got, sums = cache.attend(q.cuda(), ints(tables), ints(lengths), window=window, sums=True, longest=max(lengths), **more)
+        knobs("attention_kernel", 0)
+        knobs("attention_parts", 0)
+        check_attention(got, sums, *want, dtype, 2.0 ** -15 + (2.0 ** -11 if kernel == 2 else 0))
+
+
+@pytest.mark.parametrize("parts", [1, 5])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_over_blocks_of_far_apart_scales(dtype, kernel, parts, knobs):
+    """Values whose blocks lie far apart, the largest first, last, or seen by few of the rows; the smallest bytes."""
+    g = rng(16)
+    page, dim, n, heads, queries = 16, 96, 600, 3, 50
+    cache = M.KvCache8(38, page, 1, dim)
+    tables = sequences(g, cache, [n])
+    fill(g, cache, tables, [n])
+    q = normal(g, queries, heads, dim, dtype=dtype)
+    order = torch.from_numpy(tables[0, :38])
+    for first, middle, last in ((110, 110, 110), (123, 110, 83), (83, 110, 123), (110, 125, 110), (50, 83, 50), (103, 116, 104), (0, 1, 3), (90, 90, 1)):
+        cache.scales[order[:19], ..., 1], cache.scales[order[19:30], ..., 1], cache.scales[order[30:], ..., 1] = first, middle, last
+        knobs("attention_kernel", kernel)
+        knobs("attention_parts", parts)
+        for window in (0, 100):
+            want, total, reach, far = ref.attend_cached(to_numpy(q), *content(cache), page, tables, [n], [0, queries], window=window)
+            got = cache.attend(q.cuda(), ints(tables), ints([n]), start=ints([0, queries]), most_queries=queries, window=window, longest=n)
+            # by the largest value that a row sees: what lies far below it counts for as much as its weight's rounding, no more
+            close(got, want, dtype, (2 * (reach * 2.0 ** -16 + 2.0 ** -15 + (2.0 ** -11 if kernel == 2 else 0)) * far)[..., None])
 
 
 def test_attention_a_long_sequence_and_its_parts():

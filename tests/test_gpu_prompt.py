@@ -90,6 +90,26 @@ def test_prompts(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,lengths,window", [(96, [1030], 0), (128, [1, 1100, 40], 0), (128, [1200], 600), (96, [50, 1027, 3], 1000)])
+def test_many_rows_that_see_many_tokens(dim, lengths, window, dtype):
+    """Calls large enough for blocks of 256 rows, some heads against the reference and all of them against blocks of 128 rows."""
+    g = rng(dim + len(lengths))
+    heads, kv_heads = 128, 32
+    start = np.concatenate([[0], np.cumsum(lengths)])
+    q, k, v = (normal(g, int(start[-1]), h, dim, dtype=dtype) for h in (heads, kv_heads, kv_heads))
+    dev = [x.cuda() for x in (q, k, v)]
+    got, sums = M.attend_prompt(*dev, ints(start), longest=max(lengths), window=window, sums=True)
+    other, other_sums = M.attend_prompt(*dev, ints(start), longest=100, window=window, sums=True)
+    for h in (0, 66, 127):
+        want = packed(to_numpy(q)[:, h:h + 1], to_numpy(k)[:, h // 4:h // 4 + 1], to_numpy(v)[:, h // 4:h // 4 + 1], start, window=window)
+        for out, s in ((got, sums), (other, other_sums)):
+            check(out[:, h:h + 1], s[:, h:h + 1], *want, dtype)
+    # both are that near to the same; 1.5 * 128 products of a mean magnitude of 0.64 make scores' reach some 11, 20 at most
+    a, b = got.double(), other.double()
+    assert (a - b).norm() <= 2 * HALF[dtype] * b.norm() and (sums - other_sums).abs().max() <= 2 * (20 * 2.0 ** -16 + 20 * 2.0 ** -21 + 2.0 ** -16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_strides_streams_outputs_and_rows_of_no_sequence(dtype):
     g = rng(31)
     dim, heads, kv_heads, tokens = 96, 4, 2, 140
