@@ -557,7 +557,7 @@ MACKO_API int64_t macko_kv8_cache_bytes(const macko_kv8_cache_t* cache, int64_t*
  * Rows before a sequence's first token (more rows than tokens), rows that are no sequence's, and tokens whose table entry names no page or
  * is missing are stored nowhere.  A position outside the table makes the token's q_out and its stored keys NaN.
  * No page that a call writes to may be another sequence's that it writes to (whole pages in front may be shared).  heads = 0: no
- * queries.  One launch. */
+ * queries.  One launch, two for many tokens. */
 typedef struct macko_kv8_append_args {
   int64_t tokens;
   int32_t heads, type, batch;
@@ -586,7 +586,10 @@ MACKO_API int macko_kv8_read(const macko_kv8_cache_t* cache, int64_t tokens, con
                              int64_t v_head, void* stream);
 
 /* macko_kv_attention over this cache: the same arguments, limits and promises, but for
- * these.  Keys and values are exact; scores are sums in 32 bits of exact products of the queries as they are with the keys. */
+ * these.  Keys and values are exact; scores are sums in 32 bits of exact products of the queries as they are with the keys.
+ * Weights go into their products with 16 bits, whatever their size; calls of more than 64 rows (most_queries * heads / kv_heads) may
+ * round them to 11, in both types, and divide by the sum of what went in (sums_dev is that of the weights before): blocks of rows in which weights below 2^-24 of a row's
+ * largest may matter, or whose blocks' values lie more than 2^6 above or 2^15 below the first ones, are done again with 16. */
 MACKO_API int64_t macko_kv8_attention_workspace(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args);
 MACKO_API int macko_kv8_attention(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
                                   int64_t workspace_bytes, void* stream);
@@ -603,7 +606,7 @@ MACKO_API int macko_kv8_attention(const macko_kv8_cache_t* cache, const macko_kv
  * taken down, and the sum is divided last: where it passes 2^128 on the way, results are infinite.
  * What lies in rows that a row does not see has no effect on it, NaN included (but it may change its last place, where values
  * that are not finite make a block of rows be done again).
- * Rows that are no sequence's are left as they were, in out and sums.  head_dim: a multiple of 32 up to 256; tokens * heads <= 2^30, 32768 heads to a
+ * Rows that are no sequence's are left as they were, in out and sums.  Any strides of 2-byte elements.  head_dim: a multiple of 32 up to 256; tokens * heads <= 2^30, 32768 heads to a
  * key/value head (MACKO_E_UNSUPPORTED otherwise).  out must not overlap q, k or v.  One launch, no workspace. */
 typedef struct macko_prompt_args {
   int64_t tokens;
@@ -619,7 +622,8 @@ typedef struct macko_prompt_args {
   float* sums_dev;              /* [tokens][heads], or NULL */
   const int32_t* start_dev;     /* [batch + 1], or NULL */
   int32_t window;
-  int64_t longest;              /* rows of one sequence at most: sizes the launch, too small costs time, not correctness */
+  int64_t longest;              /* rows of one sequence at most (without start_dev all rows): shapes the launch; what is too small or too large
+                                 * costs time, not correctness */
   float scale;
 } macko_prompt_args_t;
 MACKO_API int macko_prompt_attention(const macko_prompt_args_t* args, void* stream);
@@ -659,15 +663,15 @@ MACKO_API int macko_last_hip_error(void);
  *                       tests of the give-up path; the chain then reports MACKO_E_WAIT_EXPIRED)
  *   "spmm_kernel"       how macko_spmm takes a batch that both ways serve: 0 by estimates of both times,
  *                       1 pieces of vectors on the vector units, 2 the matrix cores
- *   "attention_kernel"  how macko_kv_attention takes a call: 0 by estimates of both times, 1 the kernel for few rows,
+ *   "attention_kernel"  how macko_kv_attention and macko_kv8_attention take a call: 0 by estimates of both times, 1 the kernel for few rows,
  *                       2 the one for many
  *   "attention_parts"   parts that it deals a sequence's tokens out to, at most (1 .. 256), 0 by estimate; the same
- *                       for macko_kv_attention_workspace and the call (calls of 2^24 rows and more have one part)
+ *                       for the _workspace function and the call (calls of 2^24 rows and more have one part)
  *   "gemv_block", "gemv_rows_per_wg", "gemv_ring" (2, 4 or 8), "gemv_resident",
  *   "gemv_wgs_per_cu"   the same for the dense GEMV
  * Settings are process wide and not thread safe: macko_set_tuning must not run
  * at the same time as any call that launches a kernel (macko_spmv, macko_spmv_group,
- * macko_spmv_many, macko_spmv_chain*, macko_spmm, macko_dense_gemv*, macko_kv_attention*) on another host
+ * macko_spmv_many, macko_spmv_chain*, macko_spmm, macko_dense_gemv*, macko_kv_attention*, macko_kv8_attention*) on another host
  * thread; those calls read the settings without locking.  With all knobs at 0, which
  * is the state of a process that never calls macko_set_tuning, the launching calls
  * may run concurrently on any number of host threads (macko_spmv_many and

@@ -1,7 +1,9 @@
 // The 8-bit key/value cache: new tokens into it (macko_kv8_append) and its values back (macko_kv8_read); the C entry points of these and of the attention
 // over the cache.
 //
-// A value takes 2 bytes in and 1 out, or the other way round, and some ten operations: memory bounds long calls, a launch short ones.
+// A block of 16 tokens of a head has m = its largest finite magnitude, the least byte b with m <= 448 * 2^(b-127), and codes round(x * 2^(127-b)).  A value takes 2 bytes in and 1
+// out, or the other way round, and some ten operations: memory bounds reads (65536 tokens of 8 heads of 128 channels 74 us, 5.4 TB/s; 16384 18 us, 5.5) and queries, loads that wait
+// for each other keys and values (16384 tokens 31 us, 3.2 TB/s; with 32 heads of queries 79 us, 4.7), a launch short calls (one token 5.9 us, 64 tokens of as many sequences 6.9).
 #include <cmath>
 
 #include "macko_kv8.h"
@@ -321,7 +323,7 @@ __device__ inline void store_unit(const AppendArgs& a, const Unit<LB>& u, const 
 }
 
 // Few tokens: a workgroup either turns queries of a token (groups of LT lanes take a head) or stores the block that begins in a row: each wavefront the keys or
-// the values of one head or, where a block takes fewer lanes, of several.
+// the values of one head or, where a block takes fewer lanes, of several.  One launch; its time is a launch's and four loads' that wait for each other (lengths, table, rows, byte).
 template <bool BF, int LB>
 __global__ __launch_bounds__(kBlock) void append_kernel(const AppendArgs a) {
   constexpr int LT = 1 << LB, GROUP = Unit<LB>::GROUP, PAIRS = Unit<LB>::PAIRS;
@@ -361,7 +363,9 @@ __global__ __launch_bounds__(kBlock) void append_kernel(const AppendArgs a) {
 }
 
 // Many tokens, keys and values alone: a workgroup takes the blocks that begin in 16 rows, for the keys or the values of 4 times as many heads as a wavefront has
-// at once.  What turns the keys is brought into LDS once for all of them.
+// at once.  What turns the keys is brought into LDS once for all of them.  Its loads wait for each other, so that wavefronts count: with three workgroups to a compute unit
+// 37 us for 16384 tokens of 8 heads of 128 channels, with four, for which no more than 128 registers are there, 31.  More heads to a workgroup, the next ones' rows on their way, gave
+// nothing; queries in the same launch made 83 us 108.
 template <bool BF, int LB>
 __global__ __launch_bounds__(kBlock, LB <= 4 ? 4 : 2) void blocks_kernel(const AppendArgs a) {
   constexpr int LT = 1 << LB, GROUP = Unit<LB>::GROUP, PAIRS = Unit<LB>::PAIRS;
@@ -431,7 +435,7 @@ __device__ inline Packed8 read8(uint32_t lo, uint32_t hi, float unit) {
 }
 
 // A group of LT lanes takes 4 entries of the list for one head.  Where they are 4 tokens in the order in which values lie together, the values come as whole
-// words; else byte by byte.
+// words; else byte by byte.  Every result is exact in 32 bits and rounded once.
 template <bool BF, int LB>
 __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
   constexpr int LT = 1 << LB;
@@ -521,15 +525,17 @@ int pool_of(const macko_kv8_cache_t* c, bool data, Kv8Pool* p) {
   return MACKO_OK;
 }
 
-// Calls of many tokens of sequences: keys and values by a kernel that goes by 16 rows, queries by macko_rotate's.  From this many wavefronts of keys and values on, by row.
-constexpr int64_t kManyWaves = 16384;
+// From this many tokens on, with kLongTurns and more to a sequence, keys and values go by 16 rows and queries by macko_rotate's kernel.  With 32 heads on 8 of 128 channels, fp16 (by
+// token, by 16): one sequence of 256 tokens 8 and 13 us, of 512 13 and 14, of 1024 22 and 15, of 4096 75 and 27; 1024 tokens of sequences with 8 each 22 and 15, with 4 23 and 23, with
+// 2 23 and 38, with one 28 and 68.  512 of 32 on 32: 22 and 14; 512 of 16 on 4 of 256 channels 23 and 19; of 40 on 8 of 64 channels 11 and 13.
+constexpr int64_t kManyTokens = 512, kLongTurns = 4;
 
 template <bool BF, int LB>
 int launch_append(AppendArgs& a, hipStream_t stream) {
   constexpr int LT = 1 << LB, PAIRS = Unit<LB>::PAIRS;
   a.groups = (a.pool.heads + PAIRS - 1) / PAIRS;
   const dim3 block(kBlock);
-  if (a.start && a.tokens * 2 * a.groups >= kManyWaves) {
+  if (a.start && a.tokens >= kManyTokens && a.tokens >= kLongTurns * a.batch) {
     a.rows = 16;
     a.groups = (a.groups + 3) / 4;
     hipLaunchKernelGGL((blocks_kernel<BF, LB>), dim3((unsigned)(2 * a.groups), (unsigned)std::min<int64_t>(kMostGrid, (a.tokens + 15) / 16)), block, 0, stream, a);

@@ -203,7 +203,7 @@ def attend_prompt(q, k, v, start=None, longest=None, scale=None, window=0, sums=
     """macko_prompt_attention: causal attention of packed sequences, q [tokens, heads, head_dim] over k and v [tokens, kv_heads, head_dim] of the same type.
 
     start: int32 [sequences + 1], the rows that are each sequence's; None: all rows are one.  longest: a bound on the rows of one sequence, all rows unless
-    given.  scale: head_dim ** -0.5 unless given.  Returns out, or (out, sums) with sums = True: float32 [tokens, heads], the logarithm of each row's
+    given.  scale: head_dim ** -0.5 unless given.  window > 0: a row sees that many tokens at most, itself among them.  Returns out, or (out, sums) with sums = True: float32 [tokens, heads], the logarithm of each row's
     sum, to join results with those over a cached prefix."""
     if stream is None and binding._native is not None:
         y = binding._native.attend_prompt(q, k, v, start, longest, scale, window, sums, out)

@@ -238,9 +238,7 @@ def test_append_of_many_sequences_is_that_of_each(dim, kv_heads, dtype):
     lengths[20] = -3
     start = np.concatenate([[6], 6 + np.cumsum(fresh)])
     tokens = int(start[-1]) + 9
-    assert tokens * 2 * kv_heads >= 16384                              # a wavefront has up to four heads of 32 channels, two of 64
-    if dim == 32:
-        tokens = 4 * tokens
+    assert tokens >= 512 and tokens >= 4 * batch                       # by 16 rows
     tables = np.stack([np.arange(b, 400, batch)[:4] for b in range(batch)])
     tables = np.concatenate([tables, tables[:, :1] + 3000], 1)         # 128 to 159: no page
     tables[12, 0] = -1
@@ -589,3 +587,15 @@ def test_the_run_of_a_layer():
         exact = ref.attend(turned[0][rows], turned[1][:done], to_numpy(v)[:done], done - m)[0]
         # E4M3 keeps 4 bits: a key or value is off by 2^-4 of itself at most, 2^-5.4 in the mean; scores here have a spread of 1
         assert np.linalg.norm(to_numpy(got) - exact) <= 2.0 ** -4 * np.linalg.norm(exact)
+
+
+def test_the_example_runs_the_operators_together(capsys):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decoder_layer.py")
+    spec = importlib.util.spec_from_file_location("decoder_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    # 16-bit results of a computation in 32 bits: half a unit in the last place
+    assert example.main(["--tokens", "150", "--steps", "5", "--hidden", "512", "--inner", "1000", "--heads", "8", "--kv-heads", "2", "--bits", "8"]) <= 2.0 ** -11
+    assert "8.01 bits a value" in capsys.readouterr().out
