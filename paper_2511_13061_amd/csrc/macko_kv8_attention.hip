@@ -349,7 +349,8 @@ struct Dealt {
 // time that it takes alone, or that the workgroups of a compute unit take for one each where that is longer: from memory (5.6 TB/s, once for all rows of a sequence)
 // or on the vector units and matrix cores.  Workgroups take turns where more of them come than fit.  Joining costs a launch and the sums' way through memory.
 // Constants from 1828 timings, of 1 to 64 sequences of 1024 to 131072 tokens, 1 to 1024 rows on a key/value head of 64, 128 and 256 channels, with 1 to 128
-// parts, by both kernels where there are more than 16 rows; what it chooses took 0.7 % longer than the best of these in the mean, 20 % at worst.
+// parts, by both kernels where there are more than 16 rows; what it chooses took 0.7 % longer than the best of these in the mean, 20 % at worst.  (Wide heads by the kernel for many
+// rows: from 16 sequences of 4096 tokens with 256 and 512 rows.)
 Dealt deal(const KvAttention& a, bool many, int64_t row_blocks, int64_t units) {
   static constexpr int kTry[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
   static_assert(kMostSplits == 256, "the last one tried");
@@ -357,8 +358,8 @@ Dealt deal(const KvAttention& a, bool many, int64_t row_blocks, int64_t units) {
   const double cus = device_cu_count(), rows = (double)a.tokens * a.heads, width = a.pool.dim / 128.0;
   const bool two = row_tiles(a) == 2;
   const double begin = many ? 1.9 : 2.8, alone = many ? 4.3 * (0.4 + 0.6 * width) : (two ? 1.3 : 1.1) * (0.5 + 0.5 * width);
-  const double memory = 128.0 * a.pool.dim * 2 * cus / 5.6e6 / (double)row_blocks, work = (many ? 0.97 : two ? 0.96 : 1.03) * (0.3 + 0.7 * width);
-  const double share = many ? work : std::max(memory, work), room = many ? (a.pool.dim <= 128 ? 2 : 1) : a.pool.dim <= 64 ? 3 : a.pool.dim <= 128 ? 2 : 1;
+  const double memory = 128.0 * a.pool.dim * 2 * cus / 5.6e6 / (double)row_blocks, work = many && width > 1.0 ? 0.65 * alone : (many ? 0.97 : two ? 0.96 : 1.03) * (0.3 + 0.7 * width);
+  const double share = many ? work : std::max(memory, work), room = many ? (a.pool.dim <= 192 ? 2 : 1) : a.pool.dim <= 64 ? 3 : a.pool.dim <= 128 ? 2 : 1;
   auto time = [&](int64_t splits) {
     const double groups = (double)(others * splits) / cus, steps = (double)((units + splits - 1) / splits), busy = std::min(std::ceil(groups), room);
     const double turns = groups <= 4.0 * room ? std::ceil(groups / room) : groups / room + 0.5;

@@ -62,6 +62,16 @@ __device__ inline U2 read_turned(const uint8_t* at) {
 // NaN where one of them is.
 __device__ inline float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
+// The two numbers that lane l and lane l ^ 32 have, in both.
+struct Halves {
+  float low, high;
+};
+__device__ inline Halves halves_of(float x) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t low = both[0], high = both[1];
+  return Halves{__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+
 // The sum of a pair's two numbers and x.
 template <bool HALF>
 __device__ inline float add_pair(int pair, float x) {
@@ -316,15 +326,19 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   // ---- operands from LDS
   constexpr int kKeys = NG % 4 == 0 ? 8 : NG % 2 == 0 ? 4 : 2, kValues = NG % 4 == 0 ? 4 : NG % 2 == 0 ? 2 : 1;
   uint32_t key_of[kKeys], value_of[kValues];              // by the part of a chunk's number that is swizzled; the rest are constants
+  auto find_operands = [&](int thread) {                  // for the careful steps again, as `who`
+    const int lane = thread & 63, col = lane & 31, h = lane >> 5;
 #pragma unroll
-  for (int i = 0; i < kKeys; ++i) key_of[i] = (col * CH + key_chunk<NG>(col, 2 * i + h)) * 16;
-  if constexpr (PAGED) {
-    value_of[0] = (h * D + col) * 8;
-  } else {
-    const int w = lane & 15, token = 4 * h + (w >> 2), inner = (lane >> 4 & 1) * 2 + ((w & 3) >> 1);
+    for (int i = 0; i < kKeys; ++i) key_of[i] = (col * CH + key_chunk<NG>(col, 2 * i + h)) * 16;
+    if constexpr (PAGED) {
+      value_of[0] = (h * D + col) * 8;
+    } else {
+      const int w = lane & 15, token = 4 * h + (w >> 2), inner = (lane >> 4 & 1) * 2 + ((w & 3) >> 1);
 #pragma unroll
-    for (int i = 0; i < kValues; ++i) value_of[i] = (token * CH + value_chunk<NG>(token, 4 * i + inner)) * 16 + (w & 1) * 8;
-  }
+      for (int i = 0; i < kValues; ++i) value_of[i] = (token * CH + value_chunk<NG>(token, 4 * i + inner)) * 16 + (w & 1) * 8;
+    }
+  };
+  find_operands(thread);
   auto key_operand = [&](int buffer, int part, int s) {       // tokens 32 part + col
     return *reinterpret_cast<const V4i*>(lds + buffer * kTile + key_of[s % kKeys] + (part * 32 * CH + s / kKeys * kKeys * 2) * 16);
   };
@@ -372,7 +386,8 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   };
   // `most`: the largest lifted score of the step
   auto lift = [&](float most, float kTop, float kMost) {
-    float by = fmaxf(most, __shfl_xor(most, 32));
+    const Halves both = halves_of(most);
+    float by = fmaxf(both.low, both.high);
     if (limit > -INFINITY) by = fmaxf(by, kTop);
     if (!(by > -INFINITY)) return;
     const float to = base - (by - kTop);
@@ -474,7 +489,10 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       const int from = at + part * 32;
       V16f x = {};
 #pragma unroll
-      for (int s = 0; s < 2 * NG; ++s) x = multiply32<!BF>(key_operand(0, part, s), q[s], x);
+      for (int s = 0; s < 2 * NG; ++s) {
+        if (s % 2 == 0) __builtin_amdgcn_sched_barrier(0);          // two operands on their way, or the registers do not hold them
+        x = multiply32<!BF>(key_operand(0, part, s), q[s], x);
+      }
       if (masked) hide(x, from);
       const float unit0 = unit_of(0, 2 * part), unit1 = unit_of(0, 2 * part + 1);
       const float most = fmaxf(__builtin_fmaf(largest_of(x, 0), unit0, base), __builtin_fmaf(largest_of(x, 1), unit1, base));
@@ -540,6 +558,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
 
   begin_rows();
   if (begin < end) {
+    if (thread == 0) lds_odd[0] = 0;                      // a block of rows that is gone through again sets it
     typedef std::integral_constant<bool, true> Yes;
     typedef std::integral_constant<bool, false> No;
     look_up(begin);
@@ -629,18 +648,24 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       for (int c = 0; c < NG; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) large = fmaxf(large, fabsf(out[c][i]));
-      large = fmaxf(large, __shfl_xor(large, 32));
+      const Halves both = halves_of(large);
+      large = fmaxf(both.low, both.high);
       again = again || (limit > -INFINITY && large < far);
     }
-    if (__syncthreads_or(again)) {
+    if (__any(again) && (later(threadIdx.x) & 63) == 0) atomicOr(lds_odd, 1u);
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane((int)lds_odd[0])) {
+      __syncthreads();
       begin_rows();
       first_byte = 127;
       who = later(threadIdx.x);
+      find_operands(who);
       for (int at = begin, s = 0; at < end; at += STEP, s = s + 1 == kAhead ? 0 : s + 1) {
         if (s == 0) look_up(at);
         load_keys(at, s);
         load_values(at, BOTH ? key_block : PAGED && brings_values ? block_of(at, s) : 0);
-        if (who < 2) lds_odd[who] = 0;
+        const int clears = later(threadIdx.x);
+        if (clears < 2) lds_odd[clears] = 0;
         __syncthreads();
         store_keys(0);
         store_values(at, 0, Yes{});
@@ -651,9 +676,8 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     }
   }
 
-  float total = sum + rest, whole = full;
-  total += __shfl_xor(total, 32);
-  whole += __shfl_xor(whole, 32);
+  const Halves sums = halves_of(sum + rest), fulls = halves_of(full);
+  float total = sums.low + sums.high, whole = fulls.low + fulls.high;
   const int thread_of = later(threadIdx.x), row_of = first_row + (thread_of >> 6) * 32 + (thread_of & 31), half = thread_of >> 5 & 1;
   if (PAGED ? row_of >= total_rows : reach == 0) return;
   if (bad) total = whole = NAN;
@@ -691,7 +715,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
 }
 
 template <int NG, bool BF, bool PAGED, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, NG > 4 ? 1 : 2) void rows_kernel(const LaunchRows args) {
+__global__ __launch_bounds__(64 * WAVES, NG > 6 ? 1 : 2) void rows_kernel(const LaunchRows args) {
   extern __shared__ __align__(16) uint8_t lds[];
   constexpr int kRows = 32 * WAVES;
   const KvAttention& a = args.a;
