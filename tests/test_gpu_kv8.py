@@ -599,3 +599,54 @@ def test_the_example_runs_the_operators_together(capsys):
     # 16-bit results of a computation in 32 bits: half a unit in the last place
     assert example.main(["--tokens", "150", "--steps", "5", "--hidden", "512", "--inner", "1000", "--heads", "8", "--kv-heads", "2", "--bits", "8"]) <= 2.0 ** -11
     assert "8.01 bits a value" in capsys.readouterr().out
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [40, 700])
+def test_append_strides_streams_and_queries_in_place(tokens, dtype):
+    """Tensors off every boundary, queries over themselves, another stream, a captured call that is replayed: all as the plain call, in the pool byte by byte."""
+    g = rng(tokens)
+    page, dim, heads, kv_heads = 16, 96, 5, 8
+    tables, lengths, start = ints(np.arange(50)[None]), ints([tokens + 30]), ints([0, tokens])
+    tab, w = M.rope_table(800, 64), normal(g, dim, dtype=dtype).cuda()
+    at = torch.randint(0, 800, (tokens,), generator=g).to(torch.int32).cuda()
+    x = [normal(g, tokens, h, dim, dtype=dtype).cuda() for h in (heads, kv_heads, kv_heads)]
+    more = dict(start=start, table=tab, q_weight=w, k_weight=w, eps=1e-5)
+    first = pool(rng(1), 50, page, kv_heads, dim)
+    want = first.append(*x, at, tables, lengths, **more)
+    same = lambda cache, got: torch.equal(cache.data, first.data) and torch.equal(cache.scales, first.scales) and torch.equal(got.nan_to_num(9.0), want.nan_to_num(9.0))  # noqa: E731
+
+    def odd(t):
+        return torch.empty(tokens * (t.shape[1] + 1) * (dim + 1) + 1, dtype=dtype, device="cuda")[1:].view(tokens, t.shape[1] + 1, dim + 1)[:, :t.shape[1], :dim].copy_(t)
+
+    cache = pool(rng(1), 50, page, kv_heads, dim)
+    moved = [odd(t) for t in x]
+    got = cache.append(*moved, at, tables, lengths, q_out=moved[0], **more)
+    assert got.data_ptr() == moved[0].data_ptr() and same(cache, got)
+    cache, other = pool(rng(1), 50, page, kv_heads, dim), torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    got = cache.append(*x, at, tables, lengths, stream=other, **more)
+    torch.cuda.current_stream().wait_stream(other)
+    assert same(cache, got)
+    cache = pool(rng(1), 50, page, kv_heads, dim)
+    data, scales = cache.data.clone(), cache.scales.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = cache.append(*x, at, tables, lengths, **more)
+    for _ in range(3):
+        cache.data.copy_(data)
+        cache.scales.copy_(scales)
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(cache, got)
+    slots = ints(np.arange(50 * page)[::-1].copy())
+    plain = cache.read(slots, dtype)
+    side = cache.read(slots, dtype, stream=other)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(plain, side))
+    for bad in (dict(k=x[1].float()), dict(v=x[2][:, :3]), dict(lengths=lengths.long()), dict(start=ints([0, 1, 2])), dict(positions=at[:-1]), dict(q=x[0][:-1]), dict(tables=tables[0])):
+        call = dict(dict(q=x[0], k=x[1], v=x[2], positions=at, tables=tables, lengths=lengths), **dict(more, **bad))
+        with pytest.raises((TypeError, ValueError, M.MackoError)):
+            cache.append(**call)
