@@ -434,9 +434,9 @@ __device__ inline Packed8 read8(uint32_t lo, uint32_t hi, float unit) {
   return pack8<BF>(x);
 }
 
-// A group of LT lanes takes 4 entries of the list for one head.  Where they are 4 tokens in the order in which values lie together, the values come as whole
+// A group of LT lanes takes E entries of the list for one head.  Where there are 4 and they are 4 tokens in the order in which values lie together, the values come as whole
 // words; else byte by byte.  Every result is exact in 32 bits and rounded once.
-template <bool BF, int LB>
+template <bool BF, int LB, int E>
 __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
   constexpr int LT = 1 << LB;
   const int lane = threadIdx.x & (LT - 1), dim = a.pool.dim;
@@ -445,12 +445,12 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
     const int64_t quad = item / a.pool.heads;
     const int head = (int)(item - quad * a.pool.heads);
     if (!mine) continue;
-    int64_t block[4];
-    int at[4];
-    bool there[4], wide = true;
+    int64_t block[E];
+    int at[E];
+    bool there[E], wide = E == 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t slot = quad * 4 + i < a.tokens ? a.slots[quad * 4 + i] : -1;
+    for (int i = 0; i < E; ++i) {
+      const int64_t slot = quad * E + i < a.tokens ? a.slots[quad * E + i] : -1;
       there[i] = slot >= 0 && slot < a.slots_held;
       block[i] = there[i] ? kv8_block(a.pool, slot >> a.pool.page_bits, head, (int)(slot & ((1 << a.pool.page_bits) - 1))) : 0;
       at[i] = (int)(slot & 15);
@@ -458,10 +458,10 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
     }
     const int64_t bytes = kBlockTokens * dim;
     if (a.k) {
-      W2 word[4];
-      uint32_t byte[4];
+      W2 word[E];
+      uint32_t byte[E];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < E; ++i) {
         word[i] = W2{0, 0};
         byte[i] = 127;
         if (there[i]) {
@@ -470,26 +470,28 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (quad * 4 + i < a.tokens) *reinterpret_cast<Packed8Any*>(a.k + (quad * 4 + i) * a.k_token + head * a.k_head + lane * 8) = read8<BF>(word[i][0], word[i][1], power_of(byte[i]));
+      for (int i = 0; i < E; ++i)
+        if (quad * E + i < a.tokens) *reinterpret_cast<Packed8Any*>(a.k + (quad * E + i) * a.k_token + head * a.k_head + lane * 8) = read8<BF>(word[i][0], word[i][1], power_of(byte[i]));
     }
     if (a.v) {
-      uint32_t word[4][2] = {}, byte[4] = {127, 127, 127, 127};
+      uint32_t word[E][2] = {}, byte[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) byte[i] = 127;
       if (wide) {
         const uint8_t* const from = a.pool.codes + (block[0] * 2 + 1) * bytes + ((at[0] >> 2) * dim + lane * 8) * 4;
         const W4 w[2] = {*reinterpret_cast<const W4*>(from), *reinterpret_cast<const W4*>(from + 16)};
-        byte[0] = byte[1] = byte[2] = byte[3] = a.pool.scales[block[0] * 2 + 1];
+        const uint32_t all = a.pool.scales[block[0] * 2 + 1];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t rows4[4] = {w[h][0], w[h][1], w[h][2], w[h][3]};
           uint32_t cols[4];
           turn_words(rows4, cols);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) word[i][h] = cols[i];
+          for (int i = 0; i < E; ++i) word[i][h] = cols[i], byte[i] = all;
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < E; ++i) {
           if (!there[i]) continue;
           const uint8_t* const from = a.pool.codes + (block[i] * 2 + 1) * bytes + ((at[i] >> 2) * dim + lane * 8) * 4 + (at[i] & 3);
 #pragma unroll
@@ -498,8 +500,8 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const ReadArgs a) {
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (quad * 4 + i < a.tokens) *reinterpret_cast<Packed8Any*>(a.v + (quad * 4 + i) * a.v_token + head * a.v_head + lane * 8) = read8<BF>(word[i][0], word[i][1], power_of(byte[i]));
+      for (int i = 0; i < E; ++i)
+        if (quad * E + i < a.tokens) *reinterpret_cast<Packed8Any*>(a.v + (quad * E + i) * a.v_token + head * a.v_head + lane * 8) = read8<BF>(word[i][0], word[i][1], power_of(byte[i]));
     }
   }
 }
@@ -561,17 +563,26 @@ int launch_append_type(AppendArgs& a, hipStream_t stream) {
   }
 }
 
-template <bool BF>
-void launch_read(const ReadArgs& a, hipStream_t stream) {
+template <bool BF, int E>
+void launch_read(ReadArgs& a, hipStream_t stream) {
+  a.items = (a.tokens + E - 1) / E * a.pool.heads;
   const int bits = lane_bits_of(a.pool.dim);
   const int64_t groups = kBlock >> bits;
   const dim3 grid((unsigned)std::min(kMostBlocks, (a.items + groups - 1) / groups)), block(kBlock);
   switch (bits) {
-    case 2: hipLaunchKernelGGL((read_kernel<BF, 2>), grid, block, 0, stream, a); break;
-    case 3: hipLaunchKernelGGL((read_kernel<BF, 3>), grid, block, 0, stream, a); break;
-    case 4: hipLaunchKernelGGL((read_kernel<BF, 4>), grid, block, 0, stream, a); break;
-    default: hipLaunchKernelGGL((read_kernel<BF, 5>), grid, block, 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((read_kernel<BF, 2, E>), grid, block, 0, stream, a); break;
+    case 3: hipLaunchKernelGGL((read_kernel<BF, 3, E>), grid, block, 0, stream, a); break;
+    case 4: hipLaunchKernelGGL((read_kernel<BF, 4, E>), grid, block, 0, stream, a); break;
+    default: hipLaunchKernelGGL((read_kernel<BF, 5, E>), grid, block, 0, stream, a); break;
   }
+}
+// Few entries: one to a group of lanes, whose loads are a fourth as many.  Entries in order and in no order, one to a group and four, us: 257 of 8 heads of 256 channels 4.2, 4.2 and 4.5, 7.9;
+// 1024 of 8 of 64 3.8, 3.8 and 4.4, 7.8; of 8 of 128 (131072 lanes) 4.8, 4.9 and 4.7, 8.2; of 8 of 256 7.4, 7.4 and 5.3, 8.6.
+constexpr int64_t kFewLanes = 1 << 17;
+template <bool BF>
+void launch_read_type(ReadArgs& a, hipStream_t stream) {
+  if (a.tokens * a.pool.heads << lane_bits_of(a.pool.dim) <= kFewLanes) launch_read<BF, 1>(a, stream);
+  else launch_read<BF, 4>(a, stream);
 }
 
 // The attention's arguments are those of the 4-bit cache.
@@ -635,10 +646,10 @@ int macko_kv8_read(const macko_kv8_cache_t* cache, int64_t tokens, const int32_t
   if (tokens > INT32_MAX) return MACKO_E_UNSUPPORTED;
   if (!slots_dev || !aligned_to(slots_dev, 4) || (k_out_dev && !heads_fine(k_out_dev, k_token, k_head)) || (v_out_dev && !heads_fine(v_out_dev, v_token, v_head)))
     return MACKO_E_INVALID_ARG;
-  const ReadArgs a{pool, slots_dev, tokens, pool.pages << pool.page_bits, (tokens + 3) / 4 * pool.heads, static_cast<uint16_t*>(k_out_dev), k_token, k_head,
+  ReadArgs a{pool, slots_dev, tokens, pool.pages << pool.page_bits, 0, static_cast<uint16_t*>(k_out_dev), k_token, k_head,
                    static_cast<uint16_t*>(v_out_dev), v_token, v_head};
-  if (type == MACKO_BF16) launch_read<true>(a, static_cast<hipStream_t>(stream));
-  else launch_read<false>(a, static_cast<hipStream_t>(stream));
+  if (type == MACKO_BF16) launch_read_type<true>(a, static_cast<hipStream_t>(stream));
+  else launch_read_type<false>(a, static_cast<hipStream_t>(stream));
   MACKO_HIP_TRY(hipGetLastError());
   return MACKO_OK;
 }

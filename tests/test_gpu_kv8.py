@@ -166,6 +166,24 @@ def test_read_of_every_byte_and_code(dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,heads", [(32, 4), (64, 3), (96, 2), (160, 5), (256, 1)])
+def test_read_of_long_lists(dim, heads, dtype):
+    """Entries four to a group of lanes: in order from every place of a block on, backwards, with gaps, twice, outside the pool, an odd number of them."""
+    page, pages = 32, 20
+    g = rng(dim)
+    cache = pool(g, pages, page, heads, dim)
+    cache.scales.clamp_(100, 140)
+    every = np.arange(pages * page)
+    slots = np.concatenate([every, every[1:], every[2:-1], every[3:], every[::-1], every[::4], every[1::2], [-1, -5, pages * page, 2 ** 31 - 1, -2 ** 31], np.repeat(every, 2),
+                            torch.randperm(pages * page, generator=g).numpy()])
+    slots = np.tile(slots, -(-140000 // (slots.size * heads * 4)))[:-2]
+    assert slots.size * heads * 4 > 2 ** 17
+    for x, y in zip(cache.read(ints(slots), dtype), ref.read(*content(cache), page, slots)):
+        want = torch.from_numpy(y).float().to(dtype)                 # one rounding: every value is one of 32 bits
+        assert torch.equal(x.cpu().nan_to_num(-77.0, posinf=6e4, neginf=-6e4), want.nan_to_num(-77.0, posinf=6e4, neginf=-6e4))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_append_edges_of_codes_zeros_and_what_is_not_finite(dtype):
     """Values at the middle between two codes, the largest and smallest numbers, blocks of zeros, an infinity and a NaN among others."""
     steps = ref.STEPS
