@@ -589,7 +589,8 @@ MACKO_API int macko_kv8_read(const macko_kv8_cache_t* cache, int64_t tokens, con
  * these.  Keys and values are exact; scores are sums in 32 bits of exact products of the queries as they are with the keys.
  * Weights go into their products with 16 bits, whatever their size; calls of more than 64 rows (most_queries * heads / kv_heads) may
  * round them to 11, in both types, and divide by the sum of what went in (sums_dev is that of the weights before): blocks of rows in which weights below 2^-24 of a row's
- * largest may matter, or whose blocks' values lie more than 2^6 above or 2^15 below the first ones, are done again with 16. */
+ * largest may matter, or whose blocks' values lie more than 2^6 above or 2^15 below the first ones, are done again with 16.
+ * Rows of q that are no sequence's are left as they were, in out and sums. */
 MACKO_API int64_t macko_kv8_attention_workspace(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args);
 MACKO_API int macko_kv8_attention(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
                                   int64_t workspace_bytes, void* stream);

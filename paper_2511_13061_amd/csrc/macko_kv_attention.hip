@@ -432,6 +432,11 @@ __device__ inline void write_joined(const KvAttention& a, int64_t id, int channe
   if (a.sums && channel == 0) a.sums[id] = (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
+// A row in front of all sequences or behind them, whose parts nobody wrote.
+__device__ inline bool no_sequence(const KvAttention& a, int64_t id) {
+  return a.start && (id < (int64_t)a.start[0] * a.heads || id >= (int64_t)a.start[a.batch] * a.heads);
+}
+
 // Few splits: a wavefront has a row, a lane the maximum and the sum of one split.  512 rows of 32 heads with 64 channels in 4 parts: 96 us with the attention,
 // 111 with a workgroup a row; with more parts a row's reads take longer than a wavefront's share is worth (8 rows in 32 parts 14.6 and 13.6).
 constexpr int kFewSplits = 16;
@@ -439,7 +444,7 @@ template <int NG, bool BF>
 __global__ __launch_bounds__(256) void join_few_kernel(const KvAttention a, const Grid g) {
   constexpr int D = 32 * NG, LANES = D / 4, GROUPS = LANES > 32 ? 1 : LANES > 16 ? 2 : LANES > 8 ? 4 : 8;      // a group of lanes takes a split at a time
   const int64_t rows = a.tokens * a.heads, id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= rows) return;
+  if (id >= rows || no_sequence(a, id)) return;
   const int lane = threadIdx.x & 63, group = lane / LANES, channel = lane % LANES * 4;
   const float* const parts = g.parts + id * g.splits * D;
   const float* const ms = g.parts + rows * g.splits * D + id * g.splits * 2;
@@ -486,6 +491,7 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttention a, const Gr
   __shared__ __align__(16) float lds[GROUPS][D];
   __shared__ float weight[kMostSplits], most_of[4], total_of[4];
   const int64_t id = blockIdx.x, rows = a.tokens * a.heads;
+  if (no_sequence(a, id)) return;
   const float* const parts = g.parts + id * g.splits * D;
   const float* const ms = g.parts + rows * g.splits * D + id * g.splits * 2;
   const int mine = threadIdx.x, wave = mine >> 6, group = mine / LANES, channel = mine % LANES * 4;

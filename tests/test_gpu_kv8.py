@@ -543,6 +543,30 @@ def test_strides_streams_outputs_and_rows_of_no_sequence(dtype):
             cache.attend(**call)
 
 
+@pytest.mark.parametrize("parts", [1, 3, 40])
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_rows_of_no_sequence_stay_as_they_were(kernel, parts, knobs):
+    """In front of the first sequence and behind the last one, with results joined from parts in a workspace of any content."""
+    g = rng(32)
+    page, dim, heads, kv_heads, lengths, start = 16, 64, 6, 2, [700, 3, 900], [3, 30, 33, 60]
+    cache = pool(g, 110, page, kv_heads, dim)
+    tables = sequences(g, cache, lengths)
+    fill(g, cache, tables, lengths)
+    q = normal(g, 75, heads, dim)
+    want, total, reach, far = ref.attend_cached(to_numpy(q)[3:60], *content(cache), page, tables, lengths, [s - 3 for s in start])
+    knobs("attention_kernel", kernel)
+    knobs("attention_parts", parts)
+    for junk in (1, -1, 2 ** 30):                                      # what the allocator gives the call next
+        size = 75 * heads * 256 * (dim + 3) // 4
+        del_me = [torch.full((size // n,), junk, dtype=torch.int32, device="cuda") for n in (1, 2, 4, 8, 16)]
+        torch.cuda.synchronize()
+        del del_me
+        out = torch.full((75, heads, dim), 7.0, dtype=torch.float16, device="cuda")
+        got = cache.attend(q.cuda(), ints(tables), ints(lengths), start=ints(start), most_queries=27, longest=900, out=out)
+        assert (got[:3] == 7).all() and (got[60:] == 7).all()
+        close(got[3:60], want, torch.float16, (2 * (reach * 2.0 ** -16 + 2.0 ** -15 + (2.0 ** -11 if kernel == 2 else 0)) * far)[..., None])
+
+
 def test_a_graph_of_steps():
     """Append and attend in a captured graph, replayed with lengths that grow, with eager work between the replays."""
     g = rng(40)
