@@ -535,6 +535,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
         if (token >= end) continue;
         const uint8_t* codes = nullptr;
         if constexpr (PAGED) {
+          // the first pass has looked all of these entries up: where one names no page, nobody gets here
           const int block = token >> 4, bits = a.pool.page_bits - kBlockBits;
           codes = a.pool.data + ((((int64_t)table[block >> bits] * a.pool.heads + head) << bits) + (block & ((1 << bits) - 1))) * (32 * D) + 16 * D + (token >> 2 & 3) * 4 * D + (token & 3);
         }
@@ -657,7 +658,8 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       large = fmaxf(both.low, both.high);
       again = again || (limit > -INFINITY && large < far);
     }
-    if (__any(again) && (later(threadIdx.x) & 63) == 0) atomicOr(lds_odd, 1u);
+    // With a page missing nobody goes again: the rows are NaN as it is.  All wavefronts have looked up the same entries, so that all stay.
+    if (!bad && __any(again) && (later(threadIdx.x) & 63) == 0) atomicOr(lds_odd, 1u);
     __syncthreads();
     if (__builtin_amdgcn_readfirstlane((int)lds_odd[0])) {
       __syncthreads();

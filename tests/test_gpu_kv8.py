@@ -692,3 +692,31 @@ def test_append_strides_streams_and_queries_in_place(tokens, dtype):
         call = dict(dict(q=x[0], k=x[1], v=x[2], positions=at, tables=tables, lengths=lengths), **dict(more, **bad))
         with pytest.raises((TypeError, ValueError, M.MackoError)):
             cache.append(**call)
+
+
+@pytest.mark.parametrize("parts", [1, 4])
+@pytest.mark.parametrize("kernel", [0, 1, 2])
+@pytest.mark.parametrize("dim", [64, 128, 160])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_of_many_rows_that_need_missing_pages(dtype, dim, kernel, parts, knobs):
+    """Entries that name no page, and a table that is too short, with a page 0 whose values are not numbers: their sequences' rows are NaN, the others' as ever."""
+    g = rng(dim + 1)
+    page, heads, kv_heads, asked = 16, 4, 2, 40                        # 80 rows on a key/value head
+    lengths = [100, 130, 90, 200, 140, 60]
+    cache = pool(g, 60, page, kv_heads, dim)
+    tables = np.full((6, 13), -1)
+    for b, n in enumerate(lengths):
+        tables[b, :-(-n // page)] = 1 + np.arange(-(-n // page)) + sum(-(-m // page) for m in lengths[:b])
+    fill(g, cache, tables, lengths, dtype)
+    cache.data[0, :, :, 1] = 0x7F
+    for b, entry in ((0, -1), (1, 60), (2, 2 ** 30), (4, -2 ** 31)):
+        tables[b, 2] = entry                                           # tokens that every query sees
+    q = normal(g, 6 * asked, heads, dim, dtype=dtype)
+    start = np.arange(7) * asked
+    for table, missing in ((tables, [0, 1, 2, 4]), (tables[:, :9], [0, 1, 2, 3, 4]), (tables[:, :0], range(6))):
+        want = ref.attend_cached(to_numpy(q), *content(cache), page, table, lengths, start)
+        assert [b for b in range(6) if np.isnan(want[0][b * asked:(b + 1) * asked]).all()] == list(missing)
+        knobs("attention_kernel", kernel)
+        knobs("attention_parts", parts)
+        got, sums = cache.attend(q.cuda(), ints(table), ints(lengths), start=ints(start), most_queries=asked, longest=200, sums=True)
+        check_attention(got, sums, *want, dtype, 2.0 ** -15 + (2.0 ** -11 if kernel != 1 else 0))
