@@ -693,7 +693,10 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   const float most = limit > -INFINITY ? -base : -INFINITY;
   const int64_t part = (token * a.heads + head_of) * g.splits + split;
   const bool parted = PAGED && span.used > 1;
-  const float one = PAGED && begin < end ? power_of((uint32_t)first_byte) : 1.f, r = parted ? one : total == 0.f ? 0.f : one / total;
+  // A part whose sum is asked for has that of the weights before they are rounded, and results to match: joined, each part counts by that sum, and rounding cancels out
+  // within the part.
+  const bool whole_part = parted && a.sums && total != 0.f;
+  const float one = PAGED && begin < end ? power_of((uint32_t)first_byte) : 1.f, r = whole_part ? one * (whole / total) : parted ? one : total == 0.f ? 0.f : one / total;
   uint16_t* const dst = reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + head_of * a.out_head + half * 4;
 #pragma unroll
   for (int c = 0; c < NG; ++c) {
@@ -713,7 +716,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   if (parted) {
     float* const ms = g.parts + a.tokens * a.heads * g.splits * D + part * 2;
     ms[0] = most;
-    ms[1] = total;
+    ms[1] = whole_part ? whole : total;
     if (split == 0) used_splits(a, g)[token * a.heads + head_of] = span.used;
     return;
   }

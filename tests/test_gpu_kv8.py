@@ -720,3 +720,30 @@ def test_attention_of_many_rows_that_need_missing_pages(dtype, dim, kernel, part
         knobs("attention_parts", parts)
         got, sums = cache.attend(q.cuda(), ints(table), ints(lengths), start=ints(start), most_queries=asked, longest=200, sums=True)
         check_attention(got, sums, *want, dtype, 2.0 ** -15 + (2.0 ** -11 if kernel != 1 else 0))
+
+
+@pytest.mark.parametrize("parts", [1, 3, 256])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("dim", [64, 96, 192])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sums_are_of_the_weights_before_they_are_rounded(dtype, dim, kernel, parts, knobs):
+    """Few tokens that hold nearly all of a row's weight, none of them a power of two in units of the first large one: rounded to 11 bits their sum is off by up to 2^-11."""
+    g = rng(61)
+    page, heads, queries, n = 32, 2, 40, 2000
+    cache = M.KvCache8(-(-n // page), page, 1, dim)
+    tables = sequences(g, cache, [n])
+    k, v = torch.zeros((n, 1, dim), dtype=dtype), normal(g, n, 1, dim, dtype=dtype)
+    k[..., 0] = -8.0
+    k[10::200, :, 0], k[150::200, :, 0] = 1.0, 3.0                      # 2^2.9 to 2^4.9 times the weight of the first
+    cache.append(None, k.cuda(), v.cuda(), None, ints(tables), ints([n]), start=ints([0, n]))
+    q = torch.zeros((queries, heads, dim), dtype=dtype)
+    q[..., 0] = 1.0 + torch.arange(queries * heads).view(queries, heads) / 118.0
+    want = ref.attend_cached(to_numpy(q), *content(cache), page, tables, [n], [0, queries], scale=1.0)
+    knobs("attention_kernel", kernel)
+    knobs("attention_parts", parts)
+    call = dict(start=ints([0, queries]), most_queries=queries, scale=1.0, longest=n)
+    got, sums = cache.attend(q.cuda(), ints(tables), ints([n]), sums=True, **call)
+    for x in (got, cache.attend(q.cuda(), ints(tables), ints([n]), **call)):
+        check_attention(x, None, *want, dtype, 2.0 ** -15 + (2.0 ** -11 if kernel == 2 else 0))
+    # a weight is off by the rounding of its exponent, 8 bits in front of the point at most, and of its own, its sum by less: 2^-16 of them; the logarithm's result of at most 9 by 2^-21
+    assert np.abs(to_numpy(sums) - want[1]).max() <= 2.0 ** -15
