@@ -361,12 +361,13 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
 
   // ---- the row's state
   float base = 0.f, limit = -INFINITY;                    // what scores are lifted by, and how large they may then be; nothing seen yet: 0 and -infinity
-  float sum = 0.f, rest = 0.f, full = 0.f;                // of the weights as they are multiplied, what its roundings left out; of the weights before they are rounded
+  float sum = 0.f, rest = 0.f;                            // of the weights as they are multiplied, and what its roundings left out
+  float lost = 0.f;                                       // what the weights lost as they were rounded: little, so that a token far ahead takes nothing from the sum of all others
   V16f out[NG];
   const int want_sums_now = __builtin_amdgcn_readfirstlane(a.sums != nullptr);
   constexpr bool kSumsApart = !PAGED && NG <= 2;          // loops of their own for calls with sums: else the weights are made twice there, for want of registers
   auto begin_rows = [&] {
-    base = 0.f, limit = -INFINITY, sum = rest = full = 0.f;
+    base = 0.f, limit = -INFINITY, sum = rest = lost = 0.f;
 #pragma unroll
     for (int c = 0; c < NG; ++c) out[c] = V16f{};
   };
@@ -399,7 +400,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     by = limit > -INFINITY ? __builtin_amdgcn_exp2f(to - base) : 1.f;
     base = to;
     limit = kMost;
-    sum *= by, rest *= by, full *= by;
+    sum *= by, rest *= by, lost *= by;
 #pragma unroll
     for (int c = 0; c < NG; ++c) out[c] *= by;
   };
@@ -432,7 +433,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
         asm volatile("" : "+v"(same));                    // weights of their own: those below would be made here, not beside the products
 #pragma unroll
         for (int i = 0; i < 16 * PARTS; ++i) more += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i / 16][i % 16], units[i / 8], same));
-        full += more;
+        lost += more;                                     // less what went in, below
       }
     }
     constexpr int kKeyFlight = PAGED ? 2 : 3;             // steps of keys' operands on their way; what the registers hold
@@ -464,7 +465,8 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
         if constexpr (decltype(want_sums)::value) exact += w0 + w1;
       }
     }
-    if constexpr (decltype(want_sums)::value) full += exact;
+    if constexpr (decltype(want_sums)::value) lost += exact - more;
+    else if (!kSumsApart && want_sums_now) lost -= more;
     bring_values();
     constexpr int kFlight = 4, kAll = NG * 2 * PARTS;     // values' operands on their way
     V4i value[kFlight];
@@ -509,13 +511,13 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
         weight[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], i < 8 ? unit0 : unit1, base));
         together += weight[i];
       }
-      full += together;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         parts_of<false>(weight + 8 * e, hi[e], lo[e]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) more = add_pair<false>(lo[e][i], add_pair<false>(hi[e][i], more));
       }
+      lost += together - more;
       add_sum(more);
 #pragma unroll
       for (int c = 0; c < NG; ++c) {
@@ -683,8 +685,8 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     }
   }
 
-  const Halves sums = halves_of(sum + rest), fulls = halves_of(full);
-  float total = sums.low + sums.high, whole = fulls.low + fulls.high;
+  const Halves sums = halves_of(sum + rest), losses = halves_of(lost);
+  float total = sums.low + sums.high, whole = total + (losses.low + losses.high);      // of the weights before they are rounded
   const int thread_of = later(threadIdx.x), row_of = first_row + (thread_of >> 6) * 32 + (thread_of & 31), half = thread_of >> 5 & 1;
   if (PAGED ? row_of >= total_rows : reach == 0) return;
   if (bad) total = whole = NAN;

@@ -747,3 +747,26 @@ def test_sums_are_of_the_weights_before_they_are_rounded(dtype, dim, kernel, par
         check_attention(x, None, *want, dtype, 2.0 ** -15 + (2.0 ** -11 if kernel == 2 else 0))
     # a weight is off by the rounding of its exponent, 8 bits in front of the point at most, and of its own, its sum by less: 2^-16 of them; the logarithm's result of at most 9 by 2^-21
     assert np.abs(to_numpy(sums) - want[1]).max() <= 2.0 ** -15
+
+
+@pytest.mark.parametrize("parts", [1, 5])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sums_of_a_token_2_to_the_30_ahead_of_131072(dtype, kernel, parts, knobs):
+    """Steps of 64 tokens, 2^5 of weight to a lane, that leave a sum in 32 bits above 2^30 as it was: half of the others would be lost, 2^-14 of the sum."""
+    page, dim, n, queries = 64, 32, 131072, 70
+    cache = M.KvCache8(n // page, page, 1, dim)
+    tables = np.arange(n // page)[None]
+    k, v = torch.zeros((n, 1, dim)), torch.ones((n, 1, dim))
+    k[0, 0, 0], v[0] = 20.0, 0.0                                       # a number of E4M3
+    cache.append(None, k.to(dtype).cuda(), v.to(dtype).cuda(), None, ints(tables), ints([n]), start=ints([0, n]))
+    q = torch.zeros((queries, 1, dim))
+    q[..., 0] = 1.046875                                               # 20.9375, 2^30.2
+    knobs("attention_kernel", kernel)
+    knobs("attention_parts", parts)
+    got, sums = cache.attend(q.to(dtype).cuda(), ints(tables), ints([n]), start=ints([0, queries]), most_queries=queries, scale=1.0, longest=n, sums=True)
+    others = n - queries + np.arange(queries)[:, None].astype(np.float64)
+    top = np.exp(20.9375)
+    assert np.abs(to_numpy(sums) - np.log(top + others)).max() <= 2.0 ** -16
+    want = others / (top + others)
+    assert np.all(np.abs(to_numpy(got) - want[..., None]) <= want[..., None] * (HALF[dtype] + 2.0 ** -13) + TINY[dtype])

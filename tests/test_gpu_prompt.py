@@ -255,3 +255,18 @@ def test_a_captured_prompt():
         torch.cuda.synchronize()
         want = M.attend_prompt(q, k, v, start, sums=True)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sums_of_a_token_2_to_the_30_ahead_of_131072(dtype):
+    """Steps of 64 tokens, 2^5 of weight to a lane, that leave a sum in 32 bits above 2^30 as it was: half of the others would be lost, 2^-14 of the sum."""
+    dim, n = 32, 131072
+    q, k, v = torch.zeros((n, 1, dim)), torch.zeros((n, 1, dim)), torch.ones((n, 1, dim))
+    q[..., 0], k[0, 0, 0], v[0] = 1.0, 20.875, 0.0
+    got, sums = M.attend_prompt(*(x.to(dtype).cuda() for x in (q, k, v)), scale=1.0, sums=True)
+    # weights are e^20.875 and ones
+    top, others = np.exp(20.875), np.arange(n)[:, None]
+    assert np.abs(to_numpy(sums) - np.log(top + others)).max() <= 2.0 ** -16
+    want = others / (top + others)
+    # the rounding of the first weight, of the others, of the result
+    assert np.all(np.abs(to_numpy(got) - want[..., None]) <= 2.5 * HALF[dtype] * want[..., None] + TINY[dtype])
