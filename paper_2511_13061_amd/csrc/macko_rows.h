@@ -174,9 +174,9 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   uint32_t key_code[PAGED ? 2 * NG : 1], value_code[PAGED && BOTH ? 2 * NG : 1], key_scale = 0, value_scale = 0;
   int pages = 0;                                          // PAGED: a lane has the page of one block of the next steps
   int64_t key_block = 0;                                  // PAGED, BOTH: where the values of the keys before lie
-  uint32_t largest = 0;                                   // packed, HALF: magnitudes of values, two at a time; PAGED: a block's byte
+  uint32_t largest = PAGED ? 1 : 0;                       // packed, HALF: magnitudes of values, two at a time; PAGED: a block's byte, 0 where all values are zero
   int first_byte = 0;                                     // PAGED: what values are held relative to
-  bool wide = false;                                      // PAGED: a block's values do not fit
+  bool wide = false;                                      // PAGED: a block's byte lies too far from that one
   const int own = BOTH ? wave : wave >> 1;
   int who = thread;                                       // worked out again for the careful steps: what follows from it would hold registers until then
   const bool brings_keys = BOTH || (wave & 1) == 0, brings_values = BOTH || (wave & 1) == 1;
@@ -251,6 +251,27 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       }
     }
   };
+  // PAGED: the bytes of a word of values, 4 tokens of a channel, that some row sees.
+  auto seen_bytes = [&](int at) {
+    uint32_t mask = 0xFFFFFFFFu;
+    if (at < low || at + STEP > end) {                    // what no row sees may be anything
+      mask = 0;
+      const int first = at + (own * 4 + (who >> 4 & 3)) * 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mask |= first + i >= low && first + i < end ? 255u << 8 * i : 0u;
+    }
+    return mask;
+  };
+  // PAGED: powers of two above the first blocks' with which fp16 holds a block's values.
+  auto fits = [](int above) { return above <= 6 && above >= -15; };
+  // PAGED: whether the block has values other than zero, whose factor alone counts: that of zeros, 2^-126, is far from all others.
+  auto holds = [&](uint32_t mask) {
+    const uint32_t* const code = BOTH ? value_code : key_code;
+    uint32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < 2 * NG; ++w) any |= code[w];
+    return __any((any & mask & 0x7F7F7F7Fu) != 0) != 0;
+  };
   // CAREFUL: without what is not finite, whose tokens are marked; values of fp16 as two bf16 parts, the second in the other buffer.
   auto store_values = [&](int at, int buffer, auto careful) {
     constexpr bool CAREFUL = decltype(careful)::value;
@@ -260,17 +281,11 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       const int above = (int)value_scale - first_byte;
       const float value_unit = CAREFUL ? power_of(value_scale) : power_of((uint32_t)min(max(127 + above, 1), 254));
       if (!CAREFUL) {
-        wide = wide || above > 6 || above < -15;
+        wide = wide || !fits(above);
         largest = max(largest, value_scale);
       }
       const int n = who & 15, j = who >> 4 & 3, quad = own * 4 + j;
-      uint32_t mask = 0xFFFFFFFFu;
-      if (at < low || at + STEP > end) {                  // what no row sees may be anything
-        mask = 0;
-        const int first = at + quad * 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mask |= first + i >= low && first + i < end ? 255u << 8 * i : 0u;
-      }
+      const uint32_t mask = seen_bytes(at);
       const uint32_t* const code = BOTH ? value_code : key_code;
 #pragma unroll
       for (int w = 0; w < 2 * NG; w += 2) {               // two channels: 4 tokens each, 16 bytes together
@@ -573,12 +588,32 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     load_keys(begin, 0);
     load_values(begin, BOTH ? key_block : brings_values ? block_of(begin, 0) : 0);
     if constexpr (PAGED) {
-      if (brings_values && lane == 0) lds_word[own] = value_scale;
-      __syncthreads();
-      uint32_t byte = 0;
+      // the largest byte of the first step that has values other than zero
+      int from = begin;
+      for (int s = 0;;) {
+        if (brings_values) {
+          const bool held = holds(seen_bytes(from));
+          if (lane == 0) lds_word[own] = held ? max(value_scale, 1u) : 0u;
+        }
+        __syncthreads();
+        uint32_t byte = 0;
 #pragma unroll
-      for (int i = 0; i < STEP / 16; ++i) byte = max(byte, lds_word[i]);
-      first_byte = __builtin_amdgcn_readfirstlane((int)byte);
+        for (int i = 0; i < STEP / 16; ++i) byte = max(byte, lds_word[i]);
+        first_byte = __builtin_amdgcn_readfirstlane((int)byte);
+        from += STEP;
+        if (first_byte > 0 || from >= end) break;
+        __syncthreads();                                  // all have read the words
+        if (++s == kAhead) {
+          look_up(from);
+          s = 0;
+        }
+        load_values(from, brings_values ? block_of(from, s) : 0);
+      }
+      if (first_byte == 0) first_byte = 127;              // zeros alone
+      if (from > begin + STEP) {
+        look_up(begin);
+        load_values(begin, brings_values ? block_of(begin, 0) : 0);
+      }
     }
     int slot = 1;                                         // of the next keys' pages
     int64_t value_block = 0;
@@ -630,6 +665,21 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     };
     if (kSumsApart && a.sums) go(std::integral_constant<bool, kSumsApart>{});
     else go(No{});
+    if constexpr (PAGED) {
+      // Bytes far from the others may be those of zeros: each wavefront goes through its blocks again (looking at the values in every step took 1 to 5 % of all calls).
+      if (wide) {
+        wide = false;
+        largest = 0;
+        who = later(threadIdx.x);
+        for (int at = begin, s = 0; at < end && !wide; at += STEP, s = s + 1 == kAhead ? 0 : s + 1) {
+          if (s == 0) look_up(at);
+          load_values(at, block_of(at, s));
+          if (!holds(seen_bytes(at))) continue;
+          wide = !fits((int)value_scale - first_byte);
+          largest = max(largest, max(value_scale, 1u));
+        }
+      }
+    }
     float all = 0.f;
 #pragma unroll
     for (int c = 0; c < NG; ++c)
@@ -649,7 +699,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
       most = 0;
 #pragma unroll
       for (int i = 0; i < (PAGED ? STEP / 16 : WAVES); ++i) most = max(most, lds_word[i]);
-      float far = PAGED ? kMostCode * power_of((uint32_t)min(max(127 + (int)most - first_byte, 1), 254)) : most >= 0x7C00u ? INFINITY : to_float<false>(most);
+      float far = PAGED && most == 0 ? 0.f : PAGED ? kMostCode * power_of((uint32_t)min(max(127 + (int)most - first_byte, 1), 254)) : most >= 0x7C00u ? INFINITY : to_float<false>(most);
       far *= (float)(end - begin) * (BF ? 0x1p-25f * 0x1p9f : 0x1p-25f * 0x1p12f);
       float large = 0.f;
 #pragma unroll

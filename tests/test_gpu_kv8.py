@@ -770,3 +770,40 @@ def test_sums_of_a_token_2_to_the_30_ahead_of_131072(dtype, kernel, parts, knobs
     assert np.abs(to_numpy(sums) - np.log(top + others)).max() <= 2.0 ** -16
     want = others / (top + others)
     assert np.all(np.abs(to_numpy(got) - want[..., None]) <= want[..., None] * (HALF[dtype] + 2.0 ** -13) + TINY[dtype])
+
+
+@pytest.mark.parametrize("parts", [1, 3])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("dim", [64, 128, 160])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_blocks_of_zeros_have_no_scale(dtype, dim, kernel, parts, knobs):
+    """Values of whole blocks that are zero: whatever their byte of scale is, results are the same bit by bit."""
+    g = rng(62)
+    page, heads, queries, n = 64, 3, 40, 2300
+    cache = M.KvCache8(36, page, 1, dim)
+    tables = sequences(g, cache, [n])
+    fill(g, cache, tables, [n], dtype)
+    q = normal(g, queries, heads, dim, dtype=dtype)
+    order = torch.from_numpy(tables[0, :36]).cuda()
+    data = cache.data.clone()
+    knobs("attention_kernel", kernel)
+    knobs("attention_parts", parts)
+    for zeros in ([0], [1, 2], range(5), range(80), [70, 90, 143], [143], range(66, 144)):
+        block = torch.zeros(144, dtype=torch.bool, device="cuda")
+        block[list(zeros)] = True
+        cache.data.copy_(data)
+        codes = cache.data[order]                                      # [36 pages, 1, 4 blocks, 2, 16 dim]
+        codes[:, 0, :, 1][block.view(36, 4)] = torch.randint(0, 2, (int(block.sum()), 16 * dim), generator=g, dtype=torch.uint8).cuda() * 0x80      # of either sign
+        cache.data[order] = codes
+        got = []
+        for byte in (110, 1, 0, 30, 200):
+            scales = cache.scales[order]
+            scales[:, 0, :, 1] = torch.where(block.view(36, 4), byte, 110).to(torch.uint8)
+            cache.scales[order] = scales
+            got.append(cache.attend(q.cuda(), ints(tables), ints([n]), start=ints([0, queries]), most_queries=queries, longest=n, sums=True))
+        want = ref.attend_cached(to_numpy(q), *content(cache), page, tables, [n], [0, queries])
+        # element by element: results of some 2^-14, where fp16's numbers are 2^-24 apart, are off by 2^-25, however small they are
+        close(got[0][0], want[0], dtype, (2 * (want[2] * 2.0 ** -16 + 2.0 ** -15 + (2.0 ** -11 if kernel == 2 else 0)) * want[3])[..., None])
+        assert np.all(np.abs(to_numpy(got[0][1]) - want[1]) <= want[2] * 2.0 ** -16 + np.abs(want[1]) * 2.0 ** -21 + 2.0 ** -15)
+        for x, s in got[1:]:
+            assert torch.equal(x, got[0][0]) and torch.equal(s, got[0][1]), list(zeros)[:3]
