@@ -490,7 +490,7 @@ MACKO_API int macko_kv_read(const macko_kv_cache_t* cache, int64_t tokens, const
  * queries see may decide how a query's own are multiplied, and change its last place).  A table entry that a
  * query needs and that names no page, or is missing (length > table_width * page_size), makes its
  * results NaN, and may make those of the sequence's other queries NaN.  Rows of q that
- * are no sequence's are left with any content.
+ * are no sequence's are left as they were, in out and sums.
  * Limits (MACKO_E_UNSUPPORTED): batch <= 65535, tokens * heads <= 2^30, 32768 heads to a
  * key/value head; lengths above 2^30 count as 2^30.
  * most_queries and longest are upper bounds that size the launch (queries of one
@@ -589,8 +589,8 @@ MACKO_API int macko_kv8_read(const macko_kv8_cache_t* cache, int64_t tokens, con
  * these.  Keys and values are exact; scores are sums in 32 bits of exact products of the queries as they are with the keys.
  * Weights go into their products with 16 bits, whatever their size; calls of more than 64 rows (most_queries * heads / kv_heads) may
  * round them to 11, in both types, and divide by the sum of what went in (sums_dev is that of the weights before): blocks of rows in which weights below 2^-24 of a row's
- * largest may matter, or whose blocks' values lie more than 2^6 above or 2^15 below the first ones, are done again with 16.
- * Rows of q that are no sequence's are left as they were, in out and sums. */
+ * largest may matter, or whose blocks' values lie more than 2^6 above or 2^15 below the first ones, are done again with 16 (a block of
+ * zeros lies nowhere).  Weights go up to 2^15 there before a row's largest is taken down. */
 MACKO_API int64_t macko_kv8_attention_workspace(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args);
 MACKO_API int macko_kv8_attention(const macko_kv8_cache_t* cache, const macko_kv_attention_args_t* args, void* workspace_dev,
                                   int64_t workspace_bytes, void* stream);

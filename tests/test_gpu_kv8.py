@@ -807,3 +807,50 @@ def test_blocks_of_zeros_have_no_scale(dtype, dim, kernel, parts, knobs):
         assert np.all(np.abs(to_numpy(got[0][1]) - want[1]) <= want[2] * 2.0 ** -16 + np.abs(want[1]) * 2.0 ** -21 + 2.0 ** -15)
         for x, s in got[1:]:
             assert torch.equal(x, got[0][0]) and torch.equal(s, got[0][1]), list(zeros)[:3]
+
+
+@pytest.mark.parametrize("parts", [1, 3, 40])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("bits", [4, 8, 16])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sums_of_rows_of_no_sequence_stay_too(dtype, bits, kernel, parts, knobs):
+    """Results and sums in memory of the caller's, over both caches and packed: rows in front of the first sequence and behind the last one stay as they were."""
+    import ctypes
+
+    from paper_2511_13061_amd import kv
+    g = rng(33)
+    page, dim, heads, kv_heads, tokens, lengths, start = 16, 64, 6, 2, 75, [700, 0, 900], [3, 30, 33, 60]
+    q = normal(g, tokens, heads, dim, dtype=dtype).cuda()
+    out = torch.full((tokens, heads, dim), 7.0, dtype=dtype, device="cuda")
+    sums = torch.full((tokens, heads), 7.0, device="cuda")
+    lib, kind, stream = M.load_library(), int(dtype == torch.bfloat16), torch.cuda.current_stream().cuda_stream
+    rows = ints(start)
+    if bits == 16:
+        k, v = (normal(g, tokens, kv_heads, dim, dtype=dtype).cuda() for _ in range(2))
+        a = kv._CPrompt(tokens, heads, kv_heads, dim, kind, 3, q.data_ptr(), heads * dim, dim, k.data_ptr(), kv_heads * dim, dim, v.data_ptr(), kv_heads * dim, dim,
+                        out.data_ptr(), heads * dim, dim, sums.data_ptr(), rows.data_ptr(), 0, 30, dim ** -0.5)
+        assert lib.macko_prompt_attention(ctypes.byref(a), stream) == 0
+    else:
+        cache = (M.KvCache if bits == 4 else M.KvCache8)(110, page, kv_heads, dim)
+        tables = sequences(g, cache, lengths)
+        k, v = (normal(g, 110 * page, kv_heads, dim).cuda() for _ in range(2))
+        if bits == 4:
+            cache.append(None, k, v, None, ints(np.arange(110 * page)))
+        else:
+            cache.append(None, k, v, None, ints([range(110)]), ints([110 * page]), start=ints([0, 110 * page]))
+        table, length = ints(tables), ints(lengths)
+        a = kv._CAttention(tokens, heads, kind, 3, q.data_ptr(), heads * dim, dim, out.data_ptr(), heads * dim, dim, sums.data_ptr(), table.data_ptr(), table.stride(0),
+                           table.shape[1], length.data_ptr(), rows.data_ptr(), 27, 0, 900, dim ** -0.5)
+        name = "macko_kv_attention" if bits == 4 else "macko_kv8_attention"
+        knobs("attention_kernel", kernel)
+        knobs("attention_parts", parts)
+        size = getattr(lib, name + "_workspace")(cache._p, ctypes.byref(a))
+        assert (size > 0) == (parts > 1)
+        for junk in (1, -1, 2 ** 30):
+            work = torch.full((size // 4,), junk, dtype=torch.int32, device="cuda")
+            assert getattr(lib, name)(cache._p, ctypes.byref(a), work.data_ptr() if size else None, size, stream) == 0
+    torch.cuda.synchronize()
+    outside = torch.ones(tokens, dtype=torch.bool)
+    outside[3:60] = False
+    assert (out[outside] == 7).all() and (sums[outside] == 7).all()
+    assert not (sums[~outside] == 7).any() and not (out[~outside] == 7).all(2).any()
