@@ -748,13 +748,15 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   // A part whose sum is asked for has that of the weights before they are rounded, and results to match: joined, each part counts by that sum, and rounding cancels out
   // within the part.
   const bool whole_part = parted && a.sums && total != 0.f;
-  const float one = PAGED && begin < end ? power_of((uint32_t)first_byte) : 1.f, r = whole_part ? one * (whole / total) : parted ? one : total == 0.f ? 0.f : one / total;
+  // the power of two by itself: with 1 / total it may be less than 32 bits hold, where results are not
+  const float one = PAGED && begin < end ? power_of((uint32_t)first_byte) : 1.f, r = whole_part ? whole / total : parted ? 1.f : total == 0.f ? 0.f : 1.f / total;
   uint16_t* const dst = reinterpret_cast<uint16_t*>(a.out) + token * a.out_token + head_of * a.out_head + half * 4;
 #pragma unroll
   for (int c = 0; c < NG; ++c) {
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-      const V4f o = {out[c][i] * r, out[c][i + 1] * r, out[c][i + 2] * r, out[c][i + 3] * r};
+      V4f o = {out[c][i] * r, out[c][i + 1] * r, out[c][i + 2] * r, out[c][i + 3] * r};
+      if (PAGED) o *= one;
       const int channel = c * 32 + 2 * i;
       if (parted) {
         *reinterpret_cast<V4f*>(g.parts + part * D + half * 4 + channel) = o;

@@ -854,3 +854,24 @@ def test_sums_of_rows_of_no_sequence_stay_too(dtype, bits, kernel, parts, knobs)
     outside[3:60] = False
     assert (out[outside] == 7).all() and (sums[outside] == 7).all()
     assert not (sums[~outside] == 7).any() and not (out[~outside] == 7).all(2).any()
+
+
+@pytest.mark.parametrize("parts", [1, 5])
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("byte", [1, 6, 12, 20])
+def test_values_of_the_least_scales(byte, kernel, parts, knobs):
+    """Values near the end of bf16's range, in the mean of very many: results are far above what 32 bits leave of one over the sum of weights, times the scale."""
+    g = rng(63)
+    page, dim, n, heads, queries = 64, 64, 20000, 2, 40
+    cache = M.KvCache8(-(-n // page), page, 1, dim)
+    tables = sequences(g, cache, [n])
+    k, v = torch.zeros((n, 1, dim)), 1.0 + torch.rand((n, 1, dim), generator=g)
+    cache.append(None, k.bfloat16().cuda(), v.bfloat16().cuda(), None, ints(tables), ints([n]), start=ints([0, n]))
+    cache.scales[..., 1] = byte
+    q = normal(g, queries, heads, dim, dtype=torch.bfloat16)
+    want = ref.attend_cached(to_numpy(q), *content(cache), page, tables, [n], [0, queries])
+    knobs("attention_kernel", kernel)
+    knobs("attention_parts", parts)
+    got = cache.attend(q.cuda(), ints(tables), ints([n]), start=ints([0, queries]), most_queries=queries, longest=n)
+    # keys of zero: all weights are alike, and what they are rounded to cancels out; sums of 20000 in 32 bits
+    close(got, want[0], torch.bfloat16, np.abs(want[0]) * 2.0 ** -12)
