@@ -183,7 +183,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
   constexpr int kAhead = 64 / (STEP / 16);                // steps whose pages the lanes have
   auto look_up = [&](int at) {
     if constexpr (PAGED) {
-      const int index = min((at >> 4) + lane, last_block) >> (a.pool.page_bits - kBlockBits);
+      const int index = min((at >> 4) + (later(threadIdx.x) & 63), last_block) >> (a.pool.page_bits - kBlockBits);
       const int page = table[min(index, a.table_width - 1)];
       const bool fine = index < a.table_width && page >= 0 && page < a.pool.pages;
       bad = bad || __any(!fine);
@@ -256,7 +256,7 @@ __device__ inline void rows_block(const LaunchRows& args, uint8_t* lds, const Se
     uint32_t mask = 0xFFFFFFFFu;
     if (at < low || at + STEP > end) {                    // what no row sees may be anything
       mask = 0;
-      const int first = at + (own * 4 + (who >> 4 & 3)) * 4;
+      const int first = at + (own * 4 + (later(threadIdx.x) >> 4 & 3)) * 4;      // kept from one use to the next it would hold a register; so in look_up
 #pragma unroll
       for (int i = 0; i < 4; ++i) mask |= first + i >= low && first + i < end ? 255u << 8 * i : 0u;
     }
