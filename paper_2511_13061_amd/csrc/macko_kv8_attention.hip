@@ -10,7 +10,7 @@
 //            token's weights are those that P^T needs, and a lane's 4 tokens of a channel are a word of the cache: nothing moves between lanes.
 // The four wavefronts of a workgroup take turns along the tokens and join their sums in LDS; long sequences are split over workgroups
 // too, whose unnormalised sums a second kernel joins.
-// Memory bounds long calls: one token over 131072, 32 query heads on 8 of 128 channels, 46 us (5.8 TB/s with the joining); 64 sequences of 4096 with 32 heads of 128 channels 385 us
+// Memory bounds long calls: one token over 131072, 32 query heads on 8 of 128 channels, 46 us (5.8 TB/s with the joining; 54 from Python); 64 sequences of 4096 with 32 heads of 128 channels 385 us
 // (5.6 TB/s); 16 of 4096 tokens with 8 heads 28 us (4.7).  50 tokens take 5.5 us, a launch and the chain length, table, keys.
 #include <cmath>
 

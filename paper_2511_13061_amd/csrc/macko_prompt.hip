@@ -14,8 +14,8 @@ int launch_waves(LaunchRows& l, int64_t blocks, hipStream_t stream) {
 }
 
 // Heads of 96 and 128 channels: eight wavefronts, which bring a step's keys and values for 256 rows, where those blocks fill the device twice and rows see some 512 tokens
-// in the mean, else four, which waste less at both ends of what a block sees.  128 channels, 32 heads on 8: bf16, one sequence of 4096 tokens 160 us, 179 with four;
-// of 8192 575 and 630, of 1024 tokens 39 and 36; fp16, 12800 tokens in sequences of 2048 276 us, 293 with four; of 1024 178 and 180; of 512 140 and 128; of 64 101 and 79.
+// in the mean, else four, which waste less at both ends of what a block sees.  128 channels, 32 heads on 8: bf16, one sequence of 4096 tokens 151 us, 174 with four;
+// of 8192 543 and 610, of 1024 tokens 39 and 36; fp16, 12800 tokens in sequences of 2048 274 us, 292 with four; of 1024 181 and 180; of 512 140 and 128; of 64 101 and 79.
 template <int NG, bool BF>
 int launch_type(LaunchRows& l, hipStream_t stream) {
   const int64_t rows = l.a.tokens * l.a.shared;

@@ -11,15 +11,17 @@
 //   values   O^T += V^T P^T by mfma 32x32x16.  The lanes of S^T that hold a token's weights are those that P^T needs: nothing moves between lanes.
 // A wavefront's matrix and vector instructions are in turns in one order: the scores of the next 64 tokens between the weights of these, the maxima of those
 // between the values of these.  (One step after the other took 185 us where this took 160: 4096 tokens, 128 channels, 32 heads on 8, fp16; 365 and 327 over the 8-bit cache.)
-// Matrix cores and vector units bound it, and the clock that the card's power leaves them: packed, one sequence of 8192 tokens, 32 heads on 8, bf16: 64 channels 345 us (800 TFLOP/s),
-// 96 497 (830), 128 620 (890), 160 854 (805), 192 872 (945), 224 1554 (620), 256 1603 (686): two wavefronts of more than 192 channels do not fit a SIMD's registers; fp16 1 to
-// 6 % longer.  1024 queries on each of 2 x 8192 tokens of the 8-bit cache, 128 channels: bf16 286 us (900), fp16 300.
+// Matrix cores (43 % busy) and vector units (42 %), which a wavefront's turns overlap in part alone, bound it, at the clock of the moment (2.2 GHz, and down to 1.7 on a warm card): packed,
+// one sequence of 8192 tokens, 32 heads on 8, bf16: 32 channels 244 us (564 TFLOP/s), 64 333 (825), 96 450 (917), 128 543 (1012), 160 750 (916), 192 815 (1013), 224 1550 (620), 256 1556 (707):
+// two wavefronts of more than 192 channels do not fit a SIMD's registers; fp16 4 to 9 % longer.  (Another card: 128 channels 620 us.)  1024 queries on each of 2 x 8192 tokens of the 8-bit
+// cache, 128 channels: bf16 275 us (940), fp16 285.
 // Weights are one part of 16 bits: of bf16 (8 bits, as the results have) for packed bf16, of fp16 else (11 bits from 2^-24 of a row's maximum on), which holds cached values too,
 // with the powers of two of their blocks from 2^-15 to 2^6 of a first one's.
 // A value that is not finite would reach every row of its step, with weight 0 where it is not seen: a block of rows with results that are not numbers is gone
 // through again, carefully: such values are left out of the products and added row by row.  With fp16 weights it is gone through again too where what
 // those below fp16's normal numbers have lost may come to half a unit in the last place of a row's largest result, and where cached values do not fit;
-// there weights and packed fp16 values are two bf16 parts each.
+// there weights and packed fp16 values are two bf16 parts each.  If every block is: 8192 packed tokens of 128 channels, fp16, 586 us and 1686 with it; 1024 queries on 8192 cached
+// tokens 169 and 378 (bf16 164 and 372).
 #pragma once
 
 #include "macko_kv8_attention.h"
